@@ -1,7 +1,7 @@
 """Build ``liblionmuon.so`` in-tree for gfx950.
 
-Kernels (``csrc/kernels.hip``) are compiled by hipcc for gfx950 only; the
-host planner and C ABI (``csrc/plan.cpp``, ``csrc/api.cpp``) by g++; hipcc
+Kernels (``csrc/*.hip``) are compiled by hipcc for gfx950 only; the
+host planner and C ABI (``csrc/*.cpp``) by g++; hipcc
 links the shared library against the HIP runtime. Every call rebuilds.
 """
 from __future__ import annotations
@@ -47,12 +47,12 @@ def build(verbose: bool = False) -> str:
     os.makedirs(BUILD, exist_ok=True)
     inc = [f"-I{INCLUDE}", f"-I{CSRC}"]
     objs = []
-    for src in ("kernels.hip", "scratch.hip"):
+    for src in ("kernels.hip", "scratch.hip", "grad_rows.hip", "grad_products.hip"):
         obj = os.path.join(BUILD, src + ".o")
         _run([HIPCC, *HIP_FLAGS, *inc, "-c", os.path.join(CSRC, src), "-o", obj], verbose)
         objs.append(obj)
     cxx = shutil.which("g++") or "g++"
-    for src in ("plan.cpp", "api.cpp"):
+    for src in ("plan.cpp", "api.cpp", "grad_api.cpp"):
         obj = os.path.join(BUILD, src + ".o")
         _run([cxx, *CXX_FLAGS, *inc, "-c", os.path.join(CSRC, src), "-o", obj], verbose)
         objs.append(obj)

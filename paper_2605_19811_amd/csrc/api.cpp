@@ -12,6 +12,7 @@
 #include <string>
 #include <vector>
 
+#include "error.h"
 #include "kernels.h"
 #include "lionmuon.h"
 #include "plan.h"
@@ -887,6 +888,14 @@ lm_status step_noalloc_impl(float* const* params, const float* const* grads,
 }
 
 }  // namespace
+
+namespace lm {
+
+lm_status set_error(lm_status st, const std::string& msg) { return fail(st, msg); }
+
+int current_cus() { return current_chip().cus; }
+
+}  // namespace lm
 
 extern "C" {
 

@@ -1,0 +1,651 @@
+// gfx950 kernels of the products grouped by expert (include/lionmuon_grad.h):
+//
+//   Y = X W_e^T        rows of X and W_e along the contraction     (kRows, kRows)
+//   dX = dY W_e        W_e across it: n runs over its rows         (kRows, kCols)
+//   dW_e = dY_e^T X_e  both across it: the rows of an expert       (kCols, kCols)
+//
+// One tile kernel serves all three. The contraction goes through LDS 64 values
+// at a time, double buffered. An operand that runs along the contraction is
+// staged as rows of 64 values (128 bytes, eight 16-byte chunks XOR-swizzled by
+// row); one that runs across it as 64 rows of the tile's width, read through
+// gfx950's LDS transpose reads, so that no operand is ever transposed in memory.
+//
+// The host knows the total of rows and the number of experts, never the rows of
+// each: the grid covers the most row tiles that any split into experts can need,
+// and a workgroup finds its expert and tile from the offsets (find_tile).
+//
+// Ragged edges cost no branch in the loop: operands are read by buffer loads
+// whose descriptor ends at the last valid row, so what lies beyond reads as zero,
+// and lanes beyond the end of the contraction get an address outside.
+#include "grad_device.h"
+
+namespace lm {
+namespace {
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef f16 f16x8 __attribute__((ext_vector_type(8)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef short s16x8 __attribute__((ext_vector_type(8)));
+
+__device__ __forceinline__ f32x16 mma(s16x8 a, s16x8 b, f32x16 c, bf16) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+}
+__device__ __forceinline__ f32x16 mma(s16x8 a, s16x8 b, f32x16 c, f16) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+}
+
+template <int N>
+__device__ __forceinline__ void wait_vmcnt() {
+  // s_waitcnt fields: vmcnt[3:0] in bits 3:0, vmcnt[5:4] in 15:14; expcnt and
+  // lgkmcnt at their maxima, i.e. not waited for
+  __builtin_amdgcn_s_waitcnt((N & 15) | (7 << 4) | (15 << 8) | ((N >> 4) << 14));
+}
+
+// Workgroup barrier that orders LDS accesses only.
+__device__ __forceinline__ void lds_barrier() {
+  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+
+// Buffer descriptor of `bytes` bytes at p (raw, no stride): reads from `bytes`
+// on give zero.
+__device__ __forceinline__ u32x4 descriptor(const void* p, int64_t bytes) {
+  const uint64_t a = reinterpret_cast<uint64_t>(p);
+  u32x4 d;
+  d[0] = __builtin_amdgcn_readfirstlane(uint32_t(a));
+  d[1] = __builtin_amdgcn_readfirstlane(uint32_t(a >> 32) & 0xffffu);
+  d[2] = __builtin_amdgcn_readfirstlane(uint32_t(bytes < 0 ? 0 : (bytes > 0x7fffffff ? 0x7fffffff : bytes)));
+  d[3] = 0x00027000u;
+  return d;
+}
+constexpr uint32_t kOutside = 0x80000000u;   // beyond every descriptor
+
+// 16 bytes a lane from the buffer to LDS: lane i's land at dst + 16 i. The
+// compiler neither counts these copies nor waits for them: every wait for them is
+// explicit. (An assembly block without outputs: nothing the compiler could
+// reuse while the copy is in flight.)
+__device__ __forceinline__ void copy16(u32x4 desc, uint32_t off, const void* dst) {
+  const uint32_t d = uint32_t(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) const char*)(dst)));
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds"
+               :: "v"(off), "s"(desc), "s"(__builtin_amdgcn_readfirstlane(d)) : "memory", "m0");
+}
+
+// Expert and first row of row tile `slot` (BM rows each). Expert e's tiles
+// start at slot floor(offsets[e] / BM) + e: its ceil(rows / BM) tiles end at or
+// before the next expert's first slot, whatever the offsets, so that T / BM + count
+// slots hold every tile and one look at the offsets finds a slot's expert: the last
+// one whose first slot is not behind it. Offsets are clamped to [0, rows], so wrong
+// ones cannot lead outside. Returns false for a slot without rows.
+struct RowTile {
+  int expert, row0, end;
+};
+template <int BM>
+__device__ __forceinline__ bool find_tile(const int32_t* offsets, int experts, int rows, int slot, RowTile* t) {
+  const int lane = threadIdx.x & 63;
+  int e = -1;
+  for (int base = 0; base < experts; base += 64) {
+    const int i = base + lane;
+    const int off = min(max(offsets[min(i, experts - 1)], 0), rows);
+    const uint64_t m = __ballot(i < experts && off / BM + i <= slot);
+    if (m == 0) break;
+    e = base + 63 - __builtin_clzll(m);
+  }
+  e = __builtin_amdgcn_readfirstlane(e);
+  if (e < 0) return false;
+  const int first = min(max(offsets[e], 0), rows), end = min(max(offsets[e + 1], 0), rows);
+  t->expert = e;
+  t->row0 = __builtin_amdgcn_readfirstlane(first + (slot - (first / BM + e)) * BM);
+  t->end = __builtin_amdgcn_readfirstlane(end);
+  return t->row0 < t->end;
+}
+
+enum { kRows = 0, kCols = 1, kCodes = 2 };   // operand: along, across, across in 8 bits
+
+// Workgroup `bid` of `n` as the number of a tile, such that the workgroups of an XCD
+// (every eighth) take neighbouring tiles, which share operands in its L2.
+__device__ __forceinline__ int by_xcd(int bid, int n) {
+  const int q = n / 8, r = n % 8, x = bid % 8;
+  return x * q + min(x, r) + bid / 8;
+}
+
+// Tile `id` of m x n as (row, column), in bands of eight rows: the tiles that run
+// at the same time on an XCD form a block rather than a line.
+__device__ __forceinline__ void banded(int id, int m, int n, int* i, int* j) {
+  const int band = id / (8 * n), first = band * 8, h = min(8, m - first), r = id - band * 8 * n;
+  *j = r / h;
+  *i = first + r - *j * h;
+}
+
+// One operand's stage of 64 contraction values by a tile of W rows or columns.
+// Chunk c (16 bytes) of the stage, in the order that LDS holds them, is taken by
+// copy instruction c / 64, lane c % 64.
+template <int MODE, int W>
+struct Stage {
+  static constexpr int kChunks = W * 8;                       // of 16 bytes
+  static constexpr int kPerRow = MODE == kRows ? 8 : W / 8;   // chunks of an LDS row
+  // Physical chunk of logical chunk c in LDS row r is c ^ swz(r): 16 rows of a
+  // fragment read (kRows), or the four rows of a transpose read (kCols), fall into
+  // different banks. (Rows of 64 columns are 8 chunks: there rows go in pairs.)
+  __device__ static __forceinline__ int swz(int r) {
+    if (MODE == kRows) return (r & 7) ^ ((r >> 3) & 1);
+    return kPerRow == 8 ? ((r >> 1) & 1) * 4 : (r & 3) * 4;
+  }
+  __device__ static __forceinline__ void place(int c, int* row, int* chunk) {
+    *row = c / kPerRow;
+    *chunk = (c % kPerRow) ^ swz(*row);
+  }
+};
+
+// What a tile reads of one operand.
+struct Source {
+  const char* p;        // first element: (row 0, column 0) of the tile, contraction 0
+  int64_t ld;           // bytes
+  int rows;             // kRows: rows of the tile that exist
+  int cols;             // kCols: columns of the matrix from the tile's first on
+  int depth;            // contraction values
+};
+
+template <typename T, int MA, int MB, int BM, int BN, int WM, int WN, bool DMA>
+struct Tile {
+  static constexpr int kWavesN = BN / WN, kWaves = (BM / WM) * kWavesN, kThreads = kWaves * 64;
+  static constexpr int kMI = WM / 32, kNI = WN / 32;
+  static constexpr int kStageBytes = (BM + BN) * 128;
+  static constexpr int kLds = 2 * kStageBytes;
+  using SA = Stage<MA, BM>;
+  using SB = Stage<MB, BN>;
+
+  // Copies of one operand's stage k0 .. k0 + 63 (16-bit operands), by DMA.
+  template <int MODE, int W>
+  __device__ static __forceinline__ void copy(const Source& s, int k0, char* dst, int wave, int lane) {
+    using S = Stage<MODE, W>;
+    constexpr int kInst = S::kChunks / 64 / kWaves, kStepRows = 64 * kWaves / S::kPerRow;
+    static_assert(kInst * 64 * kWaves == S::kChunks, "whole copies");
+    int row, chunk;
+    S::place(wave * 64 + lane, &row, &chunk);
+    u32x4 d;
+    uint32_t off = uint32_t(row) * uint32_t(s.ld) + chunk * 16;
+    if constexpr (MODE == kRows) {
+      d = descriptor(s.p + int64_t(k0) * 2, (s.rows - 1) * s.ld + int64_t(s.depth - k0) * 2);
+      if (s.rows <= 0) d[2] = 0;
+      if (k0 + chunk * 8 >= s.depth) off = kOutside;
+    } else {
+      const int left = min(s.depth - k0, 64);
+      d = descriptor(s.p + int64_t(k0) * s.ld, (left - 1) * s.ld + int64_t(s.cols) * 2);
+      if (left <= 0 || s.cols <= 0) d[2] = 0;
+    }
+#pragma unroll
+    for (int q = 0; q < kInst; ++q)
+      copy16(d, off + uint32_t(q * kStepRows) * uint32_t(s.ld), dst + (q * kWaves + wave) * 1024);
+  }
+
+  // The same through registers, for rows off 16 bytes: a chunk that reaches over
+  // the end of its row goes element by element.
+  template <int MODE, int W>
+  struct Regs {
+    static constexpr int kInst = Stage<MODE, W>::kChunks / kThreads;
+    u32x4 v[kInst];
+  };
+  template <int MODE, int W>
+  __device__ static __forceinline__ void fetch(const Source& s, int k0, int tid, Regs<MODE, W>& r) {
+    using S = Stage<MODE, W>;
+#pragma unroll
+    for (int q = 0; q < Regs<MODE, W>::kInst; ++q) {
+      int row, chunk;
+      S::place(q * kThreads + tid, &row, &chunk);
+      const int first = MODE == kRows ? k0 + chunk * 8 : chunk * 8;
+      const int n = (MODE == kRows ? s.depth : s.cols) - first;
+      const bool in = MODE == kRows ? row < s.rows : k0 + row < s.depth;
+      u32x4 v = {0u, 0u, 0u, 0u};
+      if (in && n > 0) {
+        const uint16_t* p = reinterpret_cast<const uint16_t*>(s.p + int64_t(MODE == kRows ? row : k0 + row) * s.ld) + first;
+        if (n >= 8) {
+          __builtin_memcpy(&v, p, 16);
+        } else {
+#pragma unroll
+          for (int j = 0; j < 8; ++j)
+            if (j < n) v[j >> 1] |= uint32_t(p[j]) << (16 * (j & 1));
+        }
+      }
+      r.v[q] = v;
+    }
+  }
+  template <int MODE, int W>
+  __device__ static __forceinline__ void put(const Regs<MODE, W>& r, char* dst, int tid) {
+#pragma unroll
+    for (int q = 0; q < Regs<MODE, W>::kInst; ++q) *reinterpret_cast<u32x4*>(dst + (q * kThreads + tid) * 16) = r.v[q];
+  }
+
+  // A checkpoint's stage: 16 codes a load, widened to bf16 (exactly: the scale
+  // is a power of two) on the way into LDS.
+  struct CodeRegs {
+    static constexpr int kInst = BN * 64 / 16 / kThreads;
+    u32x4 v[kInst];
+    uint32_t s[kInst];
+  };
+  struct CodeSource {
+    const uint8_t* codes;      // of the tile's first column (a multiple of 128)
+    const uint8_t* scales;
+    int64_t ld, lds;
+    int cols, depth;
+  };
+  __device__ static __forceinline__ void fetch(const CodeSource& s, int k0, int tid, CodeRegs& r) {
+    constexpr int kPer = BN / 16;
+#pragma unroll
+    for (int q = 0; q < CodeRegs::kInst; ++q) {
+      const int i = q * kThreads + tid, row = i / kPer, c = (i % kPer) * 16;
+      const bool in = k0 + row < s.depth && c < s.cols;
+      const int64_t at = in ? k0 + row : 0;
+      const int col = in ? c : 0;
+      const u32x4 v = *reinterpret_cast<const u32x4*>(s.codes + at * s.ld + col);
+      const uint32_t e = s.scales[at * s.lds + col / kCkptBlock];
+      r.v[q] = in ? v : u32x4{0u, 0u, 0u, 0u};
+      r.s[q] = in ? e : 127u;
+    }
+  }
+  __device__ static __forceinline__ void put(const CodeRegs& r, char* dst, int tid) {
+    constexpr int kPer = BN / 16;
+#pragma unroll
+    for (int q = 0; q < CodeRegs::kInst; ++q) {
+      const int i = q * kThreads + tid, row = i / kPer, c = (i % kPer) * 2;   // logical chunk
+      const float scale = scale_of(r.s[q]);
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        u32x4 o;
+#pragma unroll
+        for (int w = 0; w < 2; ++w) {
+          o[2 * w] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(r.v[q][2 * h + w], scale, false));
+          o[2 * w + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(r.v[q][2 * h + w], scale, true));
+        }
+        *reinterpret_cast<u32x4*>(dst + row * (BN * 2) + ((c + h) ^ SB::swz(row)) * 16) = o;
+      }
+    }
+  }
+
+  // Fragment of 32 rows (or columns) from `w0` on and contraction values
+  // 16 kk .. + 15: lane l holds row l % 32, values 8 (l / 32) .. + 7.
+  template <int MODE, int W>
+  __device__ static __forceinline__ s16x8 fragment(const char* st, int w0, int kk, int lane) {
+    using S = Stage<MODE, W>;
+    if constexpr (MODE == kRows) {
+      const int r = w0 + (lane & 31);
+      return *reinterpret_cast<const s16x8*>(st + r * 128 + ((kk * 2 + (lane >> 5)) ^ S::swz(r)) * 16);
+    } else {
+      // two transpose reads of four contraction values each: within 16 lanes
+      // lane m points at row m / 4, columns 4 (m % 4) .. + 3, and gets column m of
+      // those four rows
+      const int g = lane >> 4, m = lane & 15;
+      const int n = w0 + 16 * (g & 1) + 4 * (m & 3), k = kk * 16 + 8 * (g >> 1) + (m >> 2);
+      const char* p = st + k * (W * 2) + (((n >> 3) ^ S::swz(k)) * 16) + (n & 7) * 2;
+      typedef __attribute__((address_space(3))) s16x4 lds4;
+      const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)(p));
+      const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)(p + 4 * (W * 2)));
+      return s16x8{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+    }
+  }
+
+  // One stage's products.
+  __device__ static __forceinline__ void compute(const char* sa, const char* sb, int wm, int wn, int lane, f32x16 (&acc)[kMI][kNI]) {
+    s16x8 fa[2][kMI], fb[2][kNI];
+    auto read = [&](int s, int kk) {
+#pragma unroll
+      for (int i = 0; i < kMI; ++i) fa[s][i] = fragment<MA, BM>(sa, wm + 32 * i, kk, lane);
+#pragma unroll
+      for (int j = 0; j < kNI; ++j) fb[s][j] = fragment<MB == kCodes ? int(kCols) : MB, BN>(sb, wn + 32 * j, kk, lane);
+    };
+    read(0, 0);
+#pragma unroll
+    for (int kk = 0; kk < 4; ++kk) {
+      if (kk + 1 < 4) read((kk + 1) & 1, kk + 1);
+#pragma unroll
+      for (int i = 0; i < kMI; ++i)
+#pragma unroll
+        for (int j = 0; j < kNI; ++j) acc[i][j] = mma(fa[kk & 1][i], fb[kk & 1][j], acc[i][j], T());
+    }
+  }
+
+  // The K loop: acc = sum over the contraction. FOLD > 0: after that many
+  // stages the accumulators are added to `out` and start again from zero (the
+  // matrix unit truncates where it adds to an accumulator: a chain of 4096
+  // values is 1e-5 off on average, chains of 256 added up in vector registers 5e-7).
+  template <int FOLD>
+  __device__ static __forceinline__ void product(const Source& a, const Source& b, const CodeSource& c, int depth, char* smem, f32x16 (&out)[kMI][kNI]) {
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int wm = (wave / kWavesN) * WM, wn = (wave % kWavesN) * WN;
+    const int nk = (depth + 63) / 64;
+    auto sa = [&](int kt) { return smem + (kt & 1) * kStageBytes; };
+    auto sb = [&](int kt) { return smem + (kt & 1) * kStageBytes + BM * 128; };
+    constexpr bool kDmaB = DMA && MB != kCodes;
+    constexpr int kModeB = MB == kCodes ? int(kCols) : MB;
+    Regs<MA, DMA ? 0 : BM> ra;
+    Regs<kModeB, (DMA || MB == kCodes) ? 0 : BN> rb;
+    CodeRegs rc;
+    auto request = [&](int kt) {
+      if constexpr (DMA) copy<MA, BM>(a, kt * 64, sa(kt), wave, lane);
+      else fetch<MA, BM>(a, kt * 64, tid, ra);
+      if constexpr (MB == kCodes) fetch(c, kt * 64, tid, rc);
+      else if constexpr (DMA) copy<kModeB, BN>(b, kt * 64, sb(kt), wave, lane);
+      else fetch<kModeB, BN>(b, kt * 64, tid, rb);
+    };
+    auto land = [&](int kt) {
+      if constexpr (!DMA) put<MA, BM>(ra, sa(kt), tid);
+      if constexpr (MB == kCodes) put(rc, sb(kt), tid);
+      else if constexpr (!DMA) put<kModeB, BN>(rb, sb(kt), tid);
+      if constexpr (DMA) wait_vmcnt<0>();
+      lds_barrier();
+    };
+    (void)kDmaB;
+    f32x16 acc[FOLD ? kMI : 1][FOLD ? kNI : 1];
+    auto zero = [](auto& x) {
+      for (auto& r : x)
+        for (auto& v : r) v = f32x16(0.0f);
+    };
+    zero(out);
+    if (nk == 0) return;
+    if constexpr (FOLD > 0) zero(acc);
+    request(0);
+    land(0);
+    int left = FOLD;
+    for (int kt = 0; kt < nk; ++kt) {
+      // into the buffer that every wave finished before the last barrier
+      if (kt + 1 < nk) request(kt + 1);
+      if constexpr (FOLD > 0) {
+        compute(sa(kt), sb(kt), wm, wn, lane, acc);
+        if (--left == 0 || kt + 1 == nk) {
+          left = FOLD;
+#pragma unroll
+          for (int i = 0; i < kMI; ++i)
+#pragma unroll
+            for (int j = 0; j < kNI; ++j) {
+              out[i][j] += acc[i][j];
+              acc[i][j] = f32x16(0.0f);
+            }
+        }
+      } else {
+        compute(sa(kt), sb(kt), wm, wn, lane, out);
+      }
+      if (kt + 1 < nk) land(kt + 1);
+    }
+  }
+};
+
+// ---------------------------------------------------------------------------
+// Y = X W_e^T and dX = dY W_e: rows of a are an expert's, k values of contraction
+// ---------------------------------------------------------------------------
+struct RowProduct {
+  const void* a;
+  const void* b;
+  void* c;
+  const int32_t* offsets;
+  int64_t lda, ldb, ldc, b_stride;    // elements
+  int rows, experts;
+  int width, depth;                   // columns of the output, contraction
+  int slots, tiles_n;
+  int vec_out;                        // rows of the output start 16-byte aligned
+};
+
+template <typename T, int MB, int BM, int BN, int WM, int WN, bool DMA>
+__global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void row_product_kernel(RowProduct g) {
+  using K = Tile<T, kRows, MB, BM, BN, WM, WN, DMA>;
+  constexpr int kStage = 32 * (WN + 8);         // elements of a wave's output staging
+  static_assert(K::kWaves * kStage * 2 <= K::kLds, "staging fits");
+  __shared__ __align__(16) char smem[K::kLds];
+  int slot, tn;
+  banded(by_xcd(blockIdx.x, gridDim.x), g.slots, g.tiles_n, &slot, &tn);
+  RowTile t;
+  if (!find_tile<BM>(g.offsets, g.experts, g.rows, slot, &t)) return;
+  const int col0 = tn * BN;
+  const T* w = static_cast<const T*>(g.b) + t.expert * g.b_stride;
+  Source a, b;
+  a.p = reinterpret_cast<const char*>(static_cast<const T*>(g.a) + t.row0 * g.lda);
+  a.ld = g.lda * 2;
+  a.rows = min(t.end - t.row0, BM);
+  a.depth = g.depth;
+  a.cols = 0;
+  b.p = reinterpret_cast<const char*>(MB == kRows ? w + col0 * g.ldb : w + col0);
+  b.ld = g.ldb * 2;
+  b.rows = min(g.width - col0, BN);
+  b.cols = g.width - col0;
+  b.depth = g.depth;
+  f32x16 acc[K::kMI][K::kNI];
+  K::template product<0>(a, b, typename K::CodeSource{}, g.depth, smem, acc);
+  lds_barrier();
+  // Output through LDS, 32 rows of a wave at a time: rows of 16-bit values
+  // leave as whole 16-byte pieces. Element r of a block is row
+  // 8 (r / 4) + 4 (lane / 32) + r % 4, column lane % 32.
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wm = (wave / K::kWavesN) * WM, wn = (wave % K::kWavesN) * WN;
+  T* st = reinterpret_cast<T*>(smem) + wave * kStage;
+  T* out = static_cast<T*>(g.c);
+#pragma unroll
+  for (int i = 0; i < K::kMI; ++i) {
+#pragma unroll
+    for (int j = 0; j < K::kNI; ++j)
+#pragma unroll
+      for (int r = 0; r < 16; ++r)
+        st[(8 * (r >> 2) + 4 * (lane >> 5) + (r & 3)) * (WN + 8) + 32 * j + (lane & 31)] = T(acc[i][j][r]);
+    // (a wave's own region: its LDS accesses are in order)
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    constexpr int kPer = WN / 8;
+#pragma unroll
+    for (int q = 0; q < 32 * kPer / 64; ++q) {
+      const int r = (q * 64 + lane) / kPer, c = (lane % kPer) * 8;
+      const int row = t.row0 + wm + 32 * i + r, col = col0 + wn + c;
+      if (row >= t.end || col >= g.width) continue;
+      const u32x4 v = *reinterpret_cast<const u32x4*>(st + r * (WN + 8) + c);
+      T* p = out + int64_t(row) * g.ldc + col;
+      if (col + 8 <= g.width) {
+        if (g.vec_out) *reinterpret_cast<u32x4*>(p) = v;
+        else __builtin_memcpy(p, &v, 16);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (col + e < g.width) p[e] = st[r * (WN + 8) + c + e];
+      }
+    }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+  }
+}
+
+// ---------------------------------------------------------------------------
+// dW_e = dY_e^T X_e
+// ---------------------------------------------------------------------------
+struct WeightProduct {
+  const void* dy;
+  const void* x;
+  CkptView kept;
+  const int32_t* offsets;
+  float* out;                         // dW, or the partials of the splits
+  int64_t lddy, ldx, ldo, o_stride;   // elements; o_stride: of an expert
+  int64_t split_stride;               // partials: of a split
+  int rows, experts, n, k;
+  int tiles_m, tiles_n, splits;
+  int accumulate;
+};
+
+template <typename T, int MB, int BM, int BN, int WM, int WN, bool DMA>
+__global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void weight_product_kernel(WeightProduct g) {
+  using K = Tile<T, kCols, MB, BM, BN, WM, WN, DMA>;
+  __shared__ __align__(16) char smem[K::kLds];
+  const int per = g.tiles_m * g.tiles_n;
+  int id = by_xcd(blockIdx.x, gridDim.x);
+  const int unit = id / per;
+  int tm, tn;
+  banded(id - unit * per, g.tiles_m, g.tiles_n, &tm, &tn);
+  const int e = unit / g.splits, s = unit - e * g.splits;
+  const int first = min(max(g.offsets[e], 0), g.rows), end = min(max(g.offsets[e + 1], 0), g.rows);
+  // this split's rows: whole stages, the same number for every split
+  const int len = max(end - first, 0);
+  const int each = ((len + 63) / 64 + g.splits - 1) / g.splits * 64;
+  const int row0 = __builtin_amdgcn_readfirstlane(first + min(s * each, len));
+  const int depth = __builtin_amdgcn_readfirstlane(min(each, first + len - row0));
+  const int m0 = tm * BM, n0 = tn * BN;
+  Source a, b;
+  typename K::CodeSource c;
+  a.p = reinterpret_cast<const char*>(static_cast<const T*>(g.dy) + row0 * g.lddy + m0);
+  a.ld = g.lddy * 2;
+  a.rows = 0;
+  a.cols = g.n - m0;
+  a.depth = depth;
+  if constexpr (MB == kCodes) {
+    c.codes = g.kept.codes + row0 * g.kept.ld_codes + n0;
+    c.scales = g.kept.scales + row0 * g.kept.ld_scales + n0 / kCkptBlock;
+    c.ld = g.kept.ld_codes;
+    c.lds = g.kept.ld_scales;
+    c.cols = g.k - n0;
+    c.depth = depth;
+  } else {
+    b.p = reinterpret_cast<const char*>(static_cast<const T*>(g.x) + row0 * g.ldx + n0);
+    b.ld = g.ldx * 2;
+    b.rows = 0;
+    b.cols = g.k - n0;
+    b.depth = depth;
+  }
+  f32x16 acc[K::kMI][K::kNI];
+  K::template product<4>(a, b, c, depth, smem, acc);
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wm = (wave / K::kWavesN) * WM, wn = (wave % K::kWavesN) * WN;
+  float* out = g.out + s * g.split_stride + e * g.o_stride;
+  // 32 lanes write 128 bytes of a row
+#pragma unroll
+  for (int i = 0; i < K::kMI; ++i)
+#pragma unroll
+    for (int j = 0; j < K::kNI; ++j) {
+      const int col = n0 + wn + 32 * j + (lane & 31);
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const int row = m0 + wm + 32 * i + 8 * (r >> 2) + 4 * (lane >> 5) + (r & 3);
+        if (row < g.n && col < g.k) {
+          float* p = out + int64_t(row) * g.ldo + col;
+          *p = g.accumulate ? *p + acc[i][j][r] : acc[i][j][r];
+        }
+      }
+    }
+}
+
+// dW = (dW +) the sum of the splits' partials, in their order: four columns a
+// thread, `blocks` workgroups a row of dW.
+__global__ __launch_bounds__(256) void weight_reduce_kernel(const float* partial, int splits, int64_t per_split, float* out, int64_t ldo, int64_t o_stride, int n, int k, int blocks, int accumulate) {
+  const int line = blockIdx.x / blocks, col = ((blockIdx.x - line * blocks) * 256 + threadIdx.x) * 4;
+  if (col >= k) return;
+  const int e = line / n, row = line - e * n;
+  const float* p = partial + int64_t(line) * k + col;
+  float* o = out + e * o_stride + row * ldo + col;
+  float v[4] = {0.f, 0.f, 0.f, 0.f};
+  const int m = min(4, k - col);
+  for (int s = 0; s < splits; ++s) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (j < m) v[j] += p[int64_t(s) * per_split + j];
+  }
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+    if (j < m) o[j] = accumulate ? o[j] + v[j] : v[j];
+}
+
+bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
+
+template <typename T, int MB, int BM, int BN, int WM, int WN>
+void run_rows(RowProduct g, bool dma, hipStream_t stream) {
+  g.slots = g.rows / BM + g.experts;
+  g.tiles_n = (g.width + BN - 1) / BN;
+  const dim3 grid(unsigned(int64_t(g.slots) * g.tiles_n));
+  constexpr int kThreads = (BM / WM) * (BN / WN) * 64;
+  if (dma) row_product_kernel<T, MB, BM, BN, WM, WN, true><<<grid, kThreads, 0, stream>>>(g);
+  else row_product_kernel<T, MB, BM, BN, WM, WN, false><<<grid, kThreads, 0, stream>>>(g);
+}
+
+template <typename T, int MB>
+void row_product(const GroupArgs& x, int width, int depth, hipStream_t stream) {
+  RowProduct g;
+  g.a = x.a;
+  g.b = x.b;
+  g.c = x.c;
+  g.offsets = x.offsets;
+  g.lda = x.lda;
+  g.ldb = x.ldb;
+  g.ldc = x.ldc;
+  g.b_stride = x.b_stride;
+  g.rows = int(x.rows);
+  g.experts = x.experts;
+  g.width = width;
+  g.depth = depth;
+  g.vec_out = aligned16(x.c) && x.ldc % 8 == 0;
+  // copies straight to LDS need rows on 16 bytes, and a contraction in whole
+  // chunks where an operand runs along it
+  const bool dma = aligned16(x.a) && aligned16(x.b) && x.lda % 8 == 0 && x.ldb % 8 == 0 && x.b_stride % 8 == 0 && depth % 8 == 0;
+  run_rows<T, MB, 128, 128, 64, 64>(g, dma, stream);
+}
+
+template <typename T, int MB>
+void weight_product(const GroupArgs& x, hipStream_t stream) {
+  constexpr int BM = 128, BN = 128;
+  WeightProduct g;
+  g.dy = x.a;
+  g.x = x.b;
+  g.kept = x.kept;
+  g.offsets = x.offsets;
+  g.lddy = x.lda;
+  g.ldx = x.ldb;
+  g.rows = int(x.rows);
+  g.experts = x.experts;
+  g.n = x.n;
+  g.k = x.k;
+  g.tiles_m = (x.n + BM - 1) / BM;
+  g.tiles_n = (x.k + BN - 1) / BN;
+  g.splits = x.splits;
+  const int64_t one = int64_t(x.n) * x.k;
+  const bool split = x.splits > 1;
+  g.out = split ? x.partial : static_cast<float*>(x.c);
+  g.ldo = split ? x.k : x.ldc;
+  g.o_stride = split ? one : x.c_stride;
+  g.split_stride = split ? one * x.experts : 0;
+  g.accumulate = split ? 0 : x.accumulate;
+  const dim3 grid(unsigned(int64_t(g.tiles_m) * g.tiles_n * x.experts * x.splits));
+  const bool dma = aligned16(x.a) && x.lda % 8 == 0 && (MB == kCodes || (aligned16(x.b) && x.ldb % 8 == 0));
+  if (dma) weight_product_kernel<T, MB, BM, BN, 64, 64, true><<<grid, 256, 0, stream>>>(g);
+  else weight_product_kernel<T, MB, BM, BN, 64, 64, false><<<grid, 256, 0, stream>>>(g);
+  if (split) {
+    const int blocks = (x.k + 1023) / 1024;
+    weight_reduce_kernel<<<dim3(unsigned(int64_t(blocks) * x.n * x.experts)), 256, 0, stream>>>(
+        x.partial, x.splits, one * x.experts, static_cast<float*>(x.c), x.ldc, x.c_stride, x.n, x.k, blocks, x.accumulate);
+  }
+}
+
+}  // namespace
+
+hipError_t launch_grouped_product(Elem t, const GroupArgs& g, hipStream_t stream) {
+  if (t == Elem::kBF16) row_product<bf16, kRows>(g, g.n, g.k, stream);
+  else row_product<f16, kRows>(g, g.n, g.k, stream);
+  return hipGetLastError();
+}
+
+hipError_t launch_grouped_input_grad(Elem t, const GroupArgs& g, hipStream_t stream) {
+  if (t == Elem::kBF16) row_product<bf16, kCols>(g, g.k, g.n, stream);
+  else row_product<f16, kCols>(g, g.k, g.n, stream);
+  return hipGetLastError();
+}
+
+hipError_t launch_grouped_weight_grad(Elem t, const GroupArgs& g, hipStream_t stream) {
+  if (g.kept.codes) weight_product<bf16, kCodes>(g, stream);
+  else if (t == Elem::kBF16) weight_product<bf16, kCols>(g, stream);
+  else weight_product<f16, kCols>(g, stream);
+  return hipGetLastError();
+}
+
+// Row ranges of an expert: as many as it takes to give every CU two tiles, of at
+// least 1024 rows each on average (a partial costs 8 bytes of traffic an
+// element, 1024 rows of contraction about 40 times that in matrix time).
+int32_t weight_grad_splits(int64_t rows, int64_t experts, int64_t n, int64_t k, int cus) {
+  const int64_t tiles = ((n + 127) / 128) * ((k + 127) / 128) * experts;
+  const int64_t want = (2 * int64_t(cus) + tiles - 1) / tiles, most = rows / experts / 1024;
+  const int64_t s = want < most ? want : most;
+  return int32_t(s < 1 ? 1 : s);
+}
+
+}  // namespace lm

@@ -1,0 +1,514 @@
+// gfx950 kernels that go along rows: 8-bit checkpoints, activation functions
+// and root-mean-square norms with their gradients (include/lionmuon_grad.h).
+// All of them are bound by HBM: each reads its inputs and writes its outputs once.
+//
+// A lane takes eight consecutive elements; the 16 lanes of a DPP row are the
+// 128 columns that share a scale, so a checkpoint's maximum is four lane
+// rotations away, without LDS, and every kernel that has a tensor in registers
+// can store its checkpoint on the way.
+#include "grad_device.h"
+
+namespace lm {
+namespace {
+
+// Maximum over the 16 lanes of a DPP row, in all of them.
+template <int CTRL>
+__device__ __forceinline__ float dpp_max(float v) {
+  return fmaxf(v, __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, 0xF, 0xF, true)));
+}
+__device__ __forceinline__ float row_max16(float v) {
+  v = dpp_max<0x128>(v);   // row_ror:8
+  v = dpp_max<0x124>(v);
+  v = dpp_max<0x122>(v);
+  return dpp_max<0x121>(v);
+}
+
+__device__ __forceinline__ bool is_finite(float v) {
+  return (__builtin_bit_cast(uint32_t, v) & 0x7f800000u) != 0x7f800000u;
+}
+
+// Codes of one block of 128 columns, eight a lane; all 16 lanes enter. Returns the
+// scale byte. 448 = 1.75 * 2^8 is e4m3's largest value: with max|x| = m 2^k,
+// 1 <= m < 2, the least e with max|x| <= 448 * 2^e is k - 8, or k - 7 for
+// m > 1.75. The scale is a power of two, so that only the rounding to three
+// fraction bits loses anything (2^-4 of the value) and the values are exact in bf16.
+__device__ __forceinline__ uint32_t encode8(const float v[8], u32x2* codes) {
+  float top = 0.0f;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) top = fmaxf(top, is_finite(v[j]) ? fabsf(v[j]) : 0.0f);
+  const uint32_t bits = __builtin_bit_cast(uint32_t, row_max16(top));
+  const int e = max(int(bits >> 23) - 127 - 8 + ((bits & 0x7fffffu) > 0x600000u ? 1 : 0), -100);
+  const float inv = scale_of(uint32_t(127 - e));
+  float s[8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) s[j] = is_finite(v[j]) ? v[j] * inv : __builtin_nanf("");
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    int c = __builtin_amdgcn_cvt_pk_fp8_f32(s[4 * h], s[4 * h + 1], 0, false);
+    c = __builtin_amdgcn_cvt_pk_fp8_f32(s[4 * h + 2], s[4 * h + 3], c, true);
+    (*codes)[h] = uint32_t(c);
+  }
+  return uint32_t(e + 127);
+}
+
+// Columns a row of codes is written to: the next multiple of 16.
+__device__ __forceinline__ int64_t padded16(int64_t cols) { return (cols + 15) & ~int64_t(15); }
+
+// Store the codes of columns c .. c + 7 of a row and, from a block's first lane, its scale.
+__device__ __forceinline__ void put8(const CkptView& k, int64_t row, int64_t c, int64_t cols, u32x2 codes, uint32_t scale) {
+  if (c < padded16(cols)) *reinterpret_cast<u32x2*>(k.codes + row * k.ld_codes + c) = codes;
+  if ((c & (kCkptBlock - 1)) == 0 && c < cols) k.scales[row * k.ld_scales + c / kCkptBlock] = uint8_t(scale);
+}
+
+// Values of columns c .. c + 7 of a checkpoint's row, of which n exist; c need
+// not be a multiple of 8 (the second half of a gated activation's input).
+__device__ __forceinline__ void get8(const CkptView& k, int64_t row, int64_t c, int64_t n, float v[8]) {
+  const uint8_t* p = k.codes + row * k.ld_codes + c;
+  u32x2 w = {0u, 0u};
+  if (n >= 8) {
+    __builtin_memcpy(&w, p, 8);
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      if (j < n) w[j >> 2] |= uint32_t(p[j]) << (8 * (j & 3));
+  }
+  const uint8_t* s = k.scales + row * k.ld_scales;
+  const int64_t last = c + (n < 8 ? n : 8) - 1;
+  const int64_t b0 = c / kCkptBlock, b1 = (last < c ? c : last) / kCkptBlock;
+  decode8(w, 1.0f, v);
+  const float s0 = n > 0 ? scale_of(s[b0]) : 0.0f, s1 = n > 0 ? scale_of(s[b1]) : 0.0f;
+  const int64_t edge = (b0 + 1) * kCkptBlock - c;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) v[j] *= j < edge ? s0 : s1;
+}
+
+// ---------------------------------------------------------------------------
+// Kernels over blocks of 128 columns: checkpoint, restore, activation
+// ---------------------------------------------------------------------------
+// A workgroup takes `per` rows; its 16 groups of 16 lanes walk their blocks.
+constexpr int kRowThreads = 256;
+
+struct BlockWalk {
+  int64_t rows, cols;
+  int32_t blocks, per;      // blocks of a row, rows of a workgroup
+};
+
+// Rows of a workgroup: four blocks for each of its groups of lanes, or one where
+// the whole tensor would not fill the chip otherwise.
+BlockWalk walk_of(int64_t rows, int64_t cols) {
+  BlockWalk w;
+  w.rows = rows;
+  w.cols = cols;
+  w.blocks = int32_t((cols + kCkptBlock - 1) / kCkptBlock);
+  const int64_t want = rows * w.blocks >= 256 * 64 ? 64 : 16;
+  w.per = int32_t(w.blocks >= want ? 1 : want / w.blocks);
+  return w;
+}
+
+template <class F>
+__device__ __forceinline__ void for_blocks(const BlockWalk& w, F f) {
+  const int64_t row0 = int64_t(blockIdx.x) * w.per;
+  const int64_t left = w.rows - row0;
+  const int total = int(left < w.per ? left : w.per) * w.blocks;
+  for (int i = threadIdx.x >> 4; i < total; i += kRowThreads / 16) {
+    const int r = i / w.blocks;
+    f(row0 + r, int64_t(i - r * w.blocks) * kCkptBlock + (threadIdx.x & 15) * 8);
+  }
+}
+
+template <typename T>
+__global__ __launch_bounds__(kRowThreads) void checkpoint_kernel(BlockWalk w, MatView x, CkptView out) {
+  for_blocks(w, [&](int64_t row, int64_t c) {
+    float v[8];
+    load8(static_cast<const T*>(x.data) + row * x.ld + c, w.cols - c, v);
+    u32x2 codes;
+    const uint32_t s = encode8(v, &codes);
+    put8(out, row, c, w.cols, codes, s);
+  });
+}
+
+template <typename T>
+__global__ __launch_bounds__(kRowThreads) void restore_kernel(BlockWalk w, CkptView k, MatView out) {
+  for_blocks(w, [&](int64_t row, int64_t c) {
+    float v[8];
+    get8(k, row, c, w.cols - c, v);
+    store8(static_cast<T*>(out.data) + row * out.ld + c, w.cols - c, v);
+  });
+}
+
+// 1 / (1 + exp(-x)); in 16-bit types by the hardware's exponential and
+// reciprocal (within 2^-21 of it), in fp32 to the last bits.
+template <typename T>
+__device__ __forceinline__ float sigmoid(float x) {
+  if constexpr (sizeof(T) == 4) return 1.0f / (1.0f + expf(-x));
+  return __builtin_amdgcn_rcpf(1.0f + __expf(-x));
+}
+
+constexpr float kGeluC = 0.7978845608028654f, kGeluA = 0.044715f;   // sqrt(2 / pi)
+enum { kGelu = 0, kSwiglu = 1 };
+
+// 0.5 (1 + tanh z) = sigmoid(2 z): no cancellation for negative x
+template <typename T>
+__device__ __forceinline__ float gelu_gate(float x) {
+  return sigmoid<T>(2.0f * kGeluC * fmaf(kGeluA * x * x, x, x));
+}
+
+// h = act(a). KEEP: with the checkpoint of a; for the gated kind the halves'
+// blocks then have to start at multiples of 128 columns.
+template <typename T, int KIND, bool KEEP>
+__global__ __launch_bounds__(kRowThreads) void activation_kernel(BlockWalk w, MatView a, MatView h, CkptView kept) {
+  const int64_t cols = w.cols;
+  for_blocks(w, [&](int64_t row, int64_t c) {
+    const T* p = static_cast<const T*>(a.data) + row * a.ld + c;
+    float x[8], u[8], o[8];
+    load8(p, cols - c, x);
+    if constexpr (KIND == kSwiglu) load8(p + cols, cols - c, u);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) o[j] = KIND == kSwiglu ? x[j] * sigmoid<T>(x[j]) * u[j] : x[j] * gelu_gate<T>(x[j]);
+    if constexpr (KEEP) {
+      u32x2 codes;
+      uint32_t s = encode8(x, &codes);
+      put8(kept, row, c, cols, codes, s);
+      if constexpr (KIND == kSwiglu) {
+        s = encode8(u, &codes);
+        put8(kept, row, cols + c, 2 * cols, codes, s);
+      }
+    }
+    store8(static_cast<T*>(h.data) + row * h.ld + c, cols - c, o);
+  });
+}
+
+// da = dh act'(a) and, where h is given, act(a) again.
+template <typename T, int KIND, bool KEPT>
+__global__ __launch_bounds__(kRowThreads) void activation_grad_kernel(BlockWalk w, MatView dh, MatView a, CkptView kept, MatView da, MatView h) {
+  const int64_t cols = w.cols;
+  for_blocks(w, [&](int64_t row, int64_t c) {
+    const int64_t n = cols - c;
+    if (n <= 0) return;
+    float x[8], u[8], d[8], o[8], dx[8], du[8];
+    load8(static_cast<const T*>(dh.data) + row * dh.ld + c, n, d);
+    if constexpr (KEPT) {
+      get8(kept, row, c, n, x);
+      if constexpr (KIND == kSwiglu) get8(kept, row, cols + c, n, u);
+    } else {
+      const T* p = static_cast<const T*>(a.data) + row * a.ld + c;
+      load8(p, n, x);
+      if constexpr (KIND == kSwiglu) load8(p + cols, n, u);
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      if constexpr (KIND == kSwiglu) {
+        const float s = sigmoid<T>(x[j]), silu = x[j] * s;
+        dx[j] = d[j] * u[j] * (s * fmaf(x[j], 1.0f - s, 1.0f));
+        du[j] = d[j] * silu;
+        o[j] = silu * u[j];
+      } else {
+        const float p = gelu_gate<T>(x[j]);
+        // d/dx sigmoid(2 z) = 2 p (1 - p) z'
+        const float z = kGeluC * fmaf(3.0f * kGeluA * x[j], x[j], 1.0f);
+        dx[j] = d[j] * fmaf(x[j] * p * (1.0f - p), 2.0f * z, p);
+        o[j] = x[j] * p;
+      }
+    }
+    T* q = static_cast<T*>(da.data) + row * da.ld + c;
+    store8(q, n, dx);
+    if constexpr (KIND == kSwiglu) store8(q + cols, n, du);
+    if (h.data) store8(static_cast<T*>(h.data) + row * h.ld + c, n, o);
+  });
+}
+
+// ---------------------------------------------------------------------------
+// Root-mean-square norm
+// ---------------------------------------------------------------------------
+// NT lanes share a row and hold it in registers, C times eight elements each:
+// a wave for rows of up to 2048 columns (four rows to a workgroup, no
+// barrier), 256 or 1024 threads for longer ones. A team walks rows with the
+// stride of the grid, so that the weights are read once a team.
+__device__ __forceinline__ float wave_sum(float v) {
+#pragma unroll
+  for (int off = 32; off >= 1; off >>= 1) v += __shfl_xor(v, off, 64);
+  return v;
+}
+
+// Sum over the NT lanes of a team, in all of them, in a fixed order. `red` is
+// used by turns (the caller passes the parity of its row), so one barrier a sum is enough.
+template <int NT>
+__device__ __forceinline__ float team_sum(float v, float (*red)[16], int parity) {
+  v = wave_sum(v);
+  if constexpr (NT == 64) return v;
+  if ((threadIdx.x & 63) == 0) red[parity][threadIdx.x >> 6] = v;
+  __syncthreads();
+  float s = 0.0f;
+#pragma unroll
+  for (int i = 0; i < NT / 64; ++i) s += red[parity][i];
+  return s;
+}
+
+template <int NT> constexpr int team_threads() { return NT == 64 ? 256 : NT; }
+
+template <typename T, int NT, int C>
+__global__ __launch_bounds__(team_threads<NT>()) void rmsnorm_kernel(NormArgs a) {
+  constexpr int kTeams = team_threads<NT>() / NT;
+  __shared__ float red[2][16];
+  const int lane = threadIdx.x % NT, team = threadIdx.x / NT;
+  const int cols = a.cols;
+  float w[C][8];
+#pragma unroll
+  for (int i = 0; i < C; ++i) {
+    const int c = (lane + i * NT) * 8;
+    load8(a.weight + c, cols - c, w[i]);
+  }
+  int parity = 0;
+  for (int64_t row = int64_t(blockIdx.x) * kTeams + team; row < a.rows; row += int64_t(gridDim.x) * kTeams) {
+    float v[C][8];
+    float ss = 0.0f;
+#pragma unroll
+    for (int i = 0; i < C; ++i) {
+      const int c = (lane + i * NT) * 8, n = cols - c;
+      load8(static_cast<const T*>(a.x.data) + row * a.x.ld + c, n, v[i]);
+      if (a.residual.data) {
+        float r[8];
+        load8(static_cast<const T*>(a.residual.data) + row * a.residual.ld + c, n, r);
+        // rounded as it is stored: the backward pass sees the same stream
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[i][j] = float(T(v[i][j] + r[j]));
+        if (a.sum.data) store8(static_cast<T*>(a.sum.data) + row * a.sum.ld + c, n, v[i]);
+      }
+#pragma unroll
+      for (int j = 0; j < 8; ++j) ss = fmaf(v[i][j], v[i][j], ss);
+    }
+    ss = team_sum<NT>(ss, red, parity);
+    parity ^= 1;
+    const float rstd = 1.0f / sqrtf(ss / float(cols) + a.eps);
+    if (a.rstd && lane == 0) a.rstd[row] = rstd;
+#pragma unroll
+    for (int i = 0; i < C; ++i) {
+      const int c = (lane + i * NT) * 8, n = cols - c;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[i][j] = v[i][j] * rstd * w[i][j];
+      if (a.y.data) store8(static_cast<T*>(a.y.data) + row * a.y.ld + c, n, v[i]);
+      if (a.kept.codes) {
+        u32x2 codes;
+        const uint32_t s = encode8(v[i], &codes);
+        put8(a.kept, row, c, cols, codes, s);
+      }
+    }
+  }
+}
+
+// dx of each row; dweight summed over the rows of a workgroup in registers (the
+// four waves of a workgroup meet in LDS), one row of partials a workgroup.
+template <typename T, int NT, int C, bool KEPT>
+__global__ __launch_bounds__(team_threads<NT>()) void rmsnorm_grad_kernel(NormArgs a) {
+  constexpr int kTeams = team_threads<NT>() / NT;
+  __shared__ float red[2][16];
+  __shared__ float sums[kTeams > 1 ? (kTeams - 1) * NT * C * 8 : 1];
+  const int lane = threadIdx.x % NT, team = threadIdx.x / NT;
+  const int cols = a.cols;
+  float w[C][8], dw[C][8];
+#pragma unroll
+  for (int i = 0; i < C; ++i) {
+    const int c = (lane + i * NT) * 8;
+    load8(a.weight + c, cols - c, w[i]);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) dw[i][j] = 0.0f;
+  }
+  int parity = 0;
+  for (int64_t row = int64_t(blockIdx.x) * kTeams + team; row < a.rows; row += int64_t(gridDim.x) * kTeams) {
+    const float rstd = a.rstd[row];
+    float h[C][8], d[C][8];
+    float dot = 0.0f;
+#pragma unroll
+    for (int i = 0; i < C; ++i) {
+      const int c = (lane + i * NT) * 8, n = cols - c;
+      if constexpr (KEPT) get8(a.kept, row, c < cols ? c : 0, n, h[i]);
+      else load8(static_cast<const T*>(a.s.data) + row * a.s.ld + c, n, h[i]);
+      load8(static_cast<const T*>(a.dy.data) + row * a.dy.ld + c, n, d[i]);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        h[i][j] *= rstd;
+        dw[i][j] = fmaf(d[i][j], h[i][j], dw[i][j]);
+        d[i][j] *= w[i][j];
+        dot = fmaf(d[i][j], h[i][j], dot);
+      }
+    }
+    if (a.dx.data) {
+      dot = team_sum<NT>(dot, red, parity) / float(cols);
+      parity ^= 1;
+#pragma unroll
+      for (int i = 0; i < C; ++i) {
+        const int c = (lane + i * NT) * 8, n = cols - c;
+        float r[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+        if (a.residual_grad.data) load8(static_cast<const T*>(a.residual_grad.data) + row * a.residual_grad.ld + c, n, r);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) r[j] = fmaf(rstd, fmaf(-h[i][j], dot, d[i][j]), r[j]);
+        store8(static_cast<T*>(a.dx.data) + row * a.dx.ld + c, n, r);
+      }
+    }
+  }
+  if (!a.dweight) return;
+  if constexpr (kTeams > 1) {
+    if (team > 0) {
+#pragma unroll
+      for (int i = 0; i < C; ++i)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) sums[(((team - 1) * C + i) * 8 + j) * NT + lane] = dw[i][j];
+    }
+    __syncthreads();
+    if (team > 0) return;
+#pragma unroll
+    for (int t = 0; t < kTeams - 1; ++t)
+#pragma unroll
+      for (int i = 0; i < C; ++i)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) dw[i][j] += sums[((t * C + i) * 8 + j) * NT + lane];
+  }
+  float* out = a.partial + int64_t(blockIdx.x) * cols;
+#pragma unroll
+  for (int i = 0; i < C; ++i) {
+    const int c = (lane + i * NT) * 8;
+    store8(out + c, cols - c, dw[i]);
+  }
+}
+
+// dweight = sum of the workgroups' partials, in a fixed order: 32 columns a
+// workgroup, each by 32 threads.
+__global__ __launch_bounds__(1024) void rmsnorm_reduce_kernel(const float* partial, int groups, int cols, float* out, int accumulate) {
+  __shared__ float red[32][33];
+  const int x = threadIdx.x & 31, y = threadIdx.x >> 5;
+  const int c = blockIdx.x * 32 + x;
+  float s = 0.0f;
+  if (c < cols) {
+#pragma unroll 8
+    for (int g = y; g < groups; g += 32) s += partial[int64_t(g) * cols + c];
+  }
+  red[y][x] = s;
+  __syncthreads();
+  if (y == 0 && c < cols) {
+    float t = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 32; ++i) t += red[i][x];
+    out[c] = accumulate ? out[c] + t : t;
+  }
+}
+
+template <class F>
+hipError_t with_type(Elem t, F f) {
+  switch (t) {
+    case Elem::kF32: f(float()); break;
+    case Elem::kBF16: f(bf16()); break;
+    case Elem::kF16: f(f16()); break;
+  }
+  return hipGetLastError();
+}
+
+template <int V> struct Int {
+  static constexpr int value = V;
+};
+
+// Lanes of a row's team and their chunks for rows of `cols` columns.
+template <class F>
+void with_team(int cols, F f) {
+  if (cols <= 512) f(Int<64>(), Int<1>());
+  else if (cols <= 1024) f(Int<64>(), Int<2>());
+  else if (cols <= 2048) f(Int<64>(), Int<4>());
+  else if (cols <= 4096) f(Int<256>(), Int<2>());
+  else if (cols <= 8192) f(Int<256>(), Int<4>());
+  else f(Int<1024>(), Int<2>());
+}
+
+// Workgroups of a norm: a row of the grid a team until every CU has eight.
+int64_t norm_groups(int64_t rows, int cols) {
+  const int64_t teams = cols <= 2048 ? 4 : 1;
+  const int64_t all = (rows + teams - 1) / teams, most = cols <= 8192 ? 2048 : 512;
+  return all < most ? all : most;
+}
+
+}  // namespace
+
+hipError_t launch_checkpoint(Elem t, MatView x, CkptView out, int64_t rows, int64_t cols, hipStream_t stream) {
+  const BlockWalk w = walk_of(rows, cols);
+  return with_type(t, [&](auto e) {
+    using T = decltype(e);
+    checkpoint_kernel<T><<<dim3(unsigned((rows + w.per - 1) / w.per)), kRowThreads, 0, stream>>>(w, x, out);
+  });
+}
+
+hipError_t launch_restore(Elem t, CkptView c, MatView out, int64_t rows, int64_t cols, hipStream_t stream) {
+  const BlockWalk w = walk_of(rows, cols);
+  return with_type(t, [&](auto e) {
+    using T = decltype(e);
+    restore_kernel<T><<<dim3(unsigned((rows + w.per - 1) / w.per)), kRowThreads, 0, stream>>>(w, c, out);
+  });
+}
+
+hipError_t launch_activation(Elem t, int kind, MatView a, MatView h, CkptView kept, int64_t rows, int64_t cols, hipStream_t stream) {
+  const BlockWalk w = walk_of(rows, cols);
+  const dim3 grid(unsigned((rows + w.per - 1) / w.per));
+  // halves that do not start with a block: the checkpoint in a launch of its own
+  const bool apart = kind == kSwiglu && cols % kCkptBlock != 0 && kept.codes;
+  hipError_t e = with_type(t, [&](auto el) {
+    using T = decltype(el);
+    const bool keep = kept.codes && !apart;
+    if (kind == kSwiglu) {
+      if (keep) activation_kernel<T, kSwiglu, true><<<grid, kRowThreads, 0, stream>>>(w, a, h, kept);
+      else activation_kernel<T, kSwiglu, false><<<grid, kRowThreads, 0, stream>>>(w, a, h, kept);
+    } else {
+      if (keep) activation_kernel<T, kGelu, true><<<grid, kRowThreads, 0, stream>>>(w, a, h, kept);
+      else activation_kernel<T, kGelu, false><<<grid, kRowThreads, 0, stream>>>(w, a, h, kept);
+    }
+  });
+  if (e == hipSuccess && apart) e = launch_checkpoint(t, a, kept, rows, 2 * cols, stream);
+  return e;
+}
+
+hipError_t launch_activation_grad(Elem t, int kind, MatView dh, MatView a, CkptView kept, MatView da, MatView h, int64_t rows, int64_t cols, hipStream_t stream) {
+  const BlockWalk w = walk_of(rows, cols);
+  const dim3 grid(unsigned((rows + w.per - 1) / w.per));
+  return with_type(t, [&](auto el) {
+    using T = decltype(el);
+    if (kind == kSwiglu) {
+      if (kept.codes) activation_grad_kernel<T, kSwiglu, true><<<grid, kRowThreads, 0, stream>>>(w, dh, a, kept, da, h);
+      else activation_grad_kernel<T, kSwiglu, false><<<grid, kRowThreads, 0, stream>>>(w, dh, a, kept, da, h);
+    } else {
+      if (kept.codes) activation_grad_kernel<T, kGelu, true><<<grid, kRowThreads, 0, stream>>>(w, dh, a, kept, da, h);
+      else activation_grad_kernel<T, kGelu, false><<<grid, kRowThreads, 0, stream>>>(w, dh, a, kept, da, h);
+    }
+  });
+}
+
+hipError_t launch_rmsnorm(Elem t, const NormArgs& a, hipStream_t stream) {
+  const dim3 grid(unsigned(norm_groups(a.rows, a.cols)));
+  return with_type(t, [&](auto el) {
+    using T = decltype(el);
+    with_team(a.cols, [&](auto nt, auto c) {
+      constexpr int kNT = decltype(nt)::value, kC = decltype(c)::value;
+      rmsnorm_kernel<T, kNT, kC><<<grid, team_threads<kNT>(), 0, stream>>>(a);
+    });
+  });
+}
+
+int64_t rmsnorm_grad_groups(int64_t rows, int64_t cols) {
+  const int64_t g = norm_groups(rows, int(cols)), most = cols <= 8192 ? 1024 : 256;
+  return g < most ? g : most;
+}
+
+hipError_t launch_rmsnorm_grad(Elem t, const NormArgs& a, hipStream_t stream) {
+  const int groups = int(rmsnorm_grad_groups(a.rows, a.cols));
+  hipError_t e = hipSuccess;
+  if (groups > 0) {
+    e = with_type(t, [&](auto el) {
+      using T = decltype(el);
+      with_team(a.cols, [&](auto nt, auto c) {
+        constexpr int kNT = decltype(nt)::value, kC = decltype(c)::value;
+        if (a.kept.codes) rmsnorm_grad_kernel<T, kNT, kC, true><<<dim3(groups), team_threads<kNT>(), 0, stream>>>(a);
+        else rmsnorm_grad_kernel<T, kNT, kC, false><<<dim3(groups), team_threads<kNT>(), 0, stream>>>(a);
+      });
+    });
+  }
+  if (e != hipSuccess || !a.dweight) return e;
+  rmsnorm_reduce_kernel<<<dim3(unsigned((a.cols + 31) / 32)), 1024, 0, stream>>>(a.partial, groups, a.cols, a.dweight, a.accumulate);
+  return hipGetLastError();
+}
+
+}  // namespace lm
