@@ -69,8 +69,10 @@ constexpr uint32_t kOutside = 0x80000000u;   // beyond every descriptor
 // reuse while the copy is in flight.)
 __device__ __forceinline__ void copy16(u32x4 desc, uint32_t off, const void* dst) {
   const uint32_t d = uint32_t(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) const char*)(dst)));
+  const u32x4 u = {uint32_t(__builtin_amdgcn_readfirstlane(desc[0])), uint32_t(__builtin_amdgcn_readfirstlane(desc[1])),
+                   uint32_t(__builtin_amdgcn_readfirstlane(desc[2])), 0x00027000u};
   asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds"
-               :: "v"(off), "s"(desc), "s"(__builtin_amdgcn_readfirstlane(d)) : "memory", "m0");
+               :: "v"(off), "s"(u), "s"(__builtin_amdgcn_readfirstlane(d)) : "memory", "m0");
 }
 
 // Expert and first row of row tile `slot` (BM rows each). Expert e's tiles
@@ -157,29 +159,40 @@ struct Tile {
   using SA = Stage<MA, BM>;
   using SB = Stage<MB, BN>;
 
-  // Copies of one operand's stage k0 .. k0 + 63 (16-bit operands), by DMA.
+  // Copies of one operand's stages (16-bit operands), by DMA: kInst copies of a
+  // wave for each stage of 64 contraction values.
   template <int MODE, int W>
-  __device__ static __forceinline__ void copy(const Source& s, int k0, char* dst, int wave, int lane) {
+  struct Copier {
     using S = Stage<MODE, W>;
-    constexpr int kInst = S::kChunks / 64 / kWaves, kStepRows = 64 * kWaves / S::kPerRow;
+    static constexpr int kInst = S::kChunks / 64 / kWaves, kStepRows = 64 * kWaves / S::kPerRow;
     static_assert(kInst * 64 * kWaves == S::kChunks, "whole copies");
-    int row, chunk;
-    S::place(wave * 64 + lane, &row, &chunk);
+    static_assert(MODE == kRows ? kStepRows % 16 == 0 : kStepRows % 4 == 0, "one swizzle for all copies of a lane");
+    Source s;
+    uint32_t off;      // the lane's byte offset in the first copy
+    int first;         // kRows: its first contraction value in the stage
     u32x4 d;
-    uint32_t off = uint32_t(row) * uint32_t(s.ld) + chunk * 16;
-    if constexpr (MODE == kRows) {
-      d = descriptor(s.p + int64_t(k0) * 2, (s.rows - 1) * s.ld + int64_t(s.depth - k0) * 2);
-      if (s.rows <= 0) d[2] = 0;
-      if (k0 + chunk * 8 >= s.depth) off = kOutside;
-    } else {
-      const int left = min(s.depth - k0, 64);
-      d = descriptor(s.p + int64_t(k0) * s.ld, (left - 1) * s.ld + int64_t(s.cols) * 2);
-      if (left <= 0 || s.cols <= 0) d[2] = 0;
+    uint32_t at;
+    __device__ __forceinline__ Copier(const Source& src, int wave, int lane) : s(src) {
+      int row, chunk;
+      S::place(wave * 64 + lane, &row, &chunk);
+      off = uint32_t(row) * uint32_t(s.ld) + chunk * 16;
+      first = chunk * 8;
     }
-#pragma unroll
-    for (int q = 0; q < kInst; ++q)
-      copy16(d, off + uint32_t(q * kStepRows) * uint32_t(s.ld), dst + (q * kWaves + wave) * 1024);
-  }
+    // Before the copies of the stage that starts with value k0.
+    __device__ __forceinline__ void start(int k0) {
+      at = off;
+      if constexpr (MODE == kRows) {
+        d = descriptor(s.p + int64_t(k0) * 2, s.rows > 0 ? (s.rows - 1) * s.ld + int64_t(s.depth - k0) * 2 : 0);
+        if (k0 + first >= s.depth) at = kOutside;
+      } else {
+        const int left = min(s.depth - k0, 64);
+        d = descriptor(s.p + int64_t(k0) * s.ld, left > 0 ? (left - 1) * s.ld + int64_t(s.cols) * 2 : 0);
+      }
+    }
+    __device__ __forceinline__ void copy(int q, char* dst, int wave) const {
+      copy16(d, at + uint32_t(q * kStepRows) * uint32_t(s.ld), dst + (q * kWaves + wave) * 1024);
+    }
+  };
 
   // The same through registers, for rows off 16 bytes: a chunk that reaches over
   // the end of its row goes element by element.
@@ -286,30 +299,16 @@ struct Tile {
     }
   }
 
-  // One stage's products.
-  __device__ static __forceinline__ void compute(const char* sa, const char* sb, int wm, int wn, int lane, f32x16 (&acc)[kMI][kNI]) {
-    s16x8 fa[2][kMI], fb[2][kNI];
-    auto read = [&](int s, int kk) {
-#pragma unroll
-      for (int i = 0; i < kMI; ++i) fa[s][i] = fragment<MA, BM>(sa, wm + 32 * i, kk, lane);
-#pragma unroll
-      for (int j = 0; j < kNI; ++j) fb[s][j] = fragment<MB == kCodes ? int(kCols) : MB, BN>(sb, wn + 32 * j, kk, lane);
-    };
-    read(0, 0);
-#pragma unroll
-    for (int kk = 0; kk < 4; ++kk) {
-      if (kk + 1 < 4) read((kk + 1) & 1, kk + 1);
-#pragma unroll
-      for (int i = 0; i < kMI; ++i)
-#pragma unroll
-        for (int j = 0; j < kNI; ++j) acc[i][j] = mma(fa[kk & 1][i], fb[kk & 1][j], acc[i][j], T());
-    }
-  }
-
-  // The K loop: acc = sum over the contraction. FOLD > 0: after that many
+  // The K loop: out = sum over the contraction. FOLD > 0: after that many
   // stages the accumulators are added to `out` and start again from zero (the
-  // matrix unit truncates where it adds to an accumulator: a chain of 4096
-  // values is 1e-5 off on average, chains of 256 added up in vector registers 5e-7).
+  // matrix unit truncates where it adds to an accumulator, which long chains show;
+  // vector additions round).
+  //
+  // A stage is four steps of 16 values. The fragments of a step are read while the
+  // step before is multiplied, across stages too: one barrier a stage, before its
+  // last step, says that every wave has read the stage (its buffer takes the stage after
+  // the next) and that the next one has landed. Copies and fragment reads are
+  // placed one behind each MFMA, so that the matrix unit never waits for a batch of them.
   template <int FOLD>
   __device__ static __forceinline__ void product(const Source& a, const Source& b, const CodeSource& c, int depth, char* smem, f32x16 (&out)[kMI][kNI]) {
     const int tid = threadIdx.x, lane = tid & 63;
@@ -318,26 +317,34 @@ struct Tile {
     const int nk = (depth + 63) / 64;
     auto sa = [&](int kt) { return smem + (kt & 1) * kStageBytes; };
     auto sb = [&](int kt) { return smem + (kt & 1) * kStageBytes + BM * 128; };
-    constexpr bool kDmaB = DMA && MB != kCodes;
     constexpr int kModeB = MB == kCodes ? int(kCols) : MB;
+    constexpr bool kDmaB = DMA && MB != kCodes;
+    constexpr int kCopiesA = DMA ? Copier<MA, BM>::kInst : 0, kCopiesB = kDmaB ? Copier<kModeB, BN>::kInst : 0;
+    constexpr int kCopies = kCopiesA + kCopiesB;
+    Copier<MA, BM> ca(a, wave, lane);
+    Copier<kModeB, BN> cb(b, wave, lane);
     Regs<MA, DMA ? 0 : BM> ra;
     Regs<kModeB, (DMA || MB == kCodes) ? 0 : BN> rb;
     CodeRegs rc;
-    auto request = [&](int kt) {
-      if constexpr (DMA) copy<MA, BM>(a, kt * 64, sa(kt), wave, lane);
-      else fetch<MA, BM>(a, kt * 64, tid, ra);
+    // stages that go through registers: loaded one stage ahead of the write to LDS
+    auto load = [&](int kt) {
+      if constexpr (!DMA) fetch<MA, BM>(a, kt * 64, tid, ra);
       if constexpr (MB == kCodes) fetch(c, kt * 64, tid, rc);
-      else if constexpr (DMA) copy<kModeB, BN>(b, kt * 64, sb(kt), wave, lane);
-      else fetch<kModeB, BN>(b, kt * 64, tid, rb);
+      else if constexpr (!DMA) fetch<kModeB, BN>(b, kt * 64, tid, rb);
     };
-    auto land = [&](int kt) {
+    auto write = [&](int kt) {
       if constexpr (!DMA) put<MA, BM>(ra, sa(kt), tid);
       if constexpr (MB == kCodes) put(rc, sb(kt), tid);
       else if constexpr (!DMA) put<kModeB, BN>(rb, sb(kt), tid);
-      if constexpr (DMA) wait_vmcnt<0>();
-      lds_barrier();
     };
-    (void)kDmaB;
+    auto start = [&](int kt) {
+      if constexpr (DMA) ca.start(kt * 64);
+      if constexpr (kDmaB) cb.start(kt * 64);
+    };
+    auto copy = [&](int kt, int q) {
+      if (q < kCopiesA) ca.copy(q, sa(kt), wave);
+      else cb.copy(q - kCopiesA, sb(kt), wave);
+    };
     f32x16 acc[FOLD ? kMI : 1][FOLD ? kNI : 1];
     auto zero = [](auto& x) {
       for (auto& r : x)
@@ -345,30 +352,76 @@ struct Tile {
     };
     zero(out);
     if (nk == 0) return;
-    if constexpr (FOLD > 0) zero(acc);
-    request(0);
-    land(0);
-    int left = FOLD;
-    for (int kt = 0; kt < nk; ++kt) {
-      // into the buffer that every wave finished before the last barrier
-      if (kt + 1 < nk) request(kt + 1);
-      if constexpr (FOLD > 0) {
-        compute(sa(kt), sb(kt), wm, wn, lane, acc);
-        if (--left == 0 || kt + 1 == nk) {
-          left = FOLD;
 #pragma unroll
-          for (int i = 0; i < kMI; ++i)
+    for (int kt = 0; kt < 2; ++kt) {
+      if (kt < nk) {
+        start(kt);
 #pragma unroll
-            for (int j = 0; j < kNI; ++j) {
-              out[i][j] += acc[i][j];
-              acc[i][j] = f32x16(0.0f);
-            }
-        }
-      } else {
-        compute(sa(kt), sb(kt), wm, wn, lane, out);
+        for (int q = 0; q < kCopies; ++q) copy(kt, q);
+        load(kt);
+        write(kt);
       }
-      if (kt + 1 < nk) land(kt + 1);
     }
+    if (2 < nk) load(2);
+    wait_vmcnt<0>();
+    lds_barrier();
+    s16x8 fa[2][kMI], fb[2][kNI];
+    // fragment f of step kk (0..3) of stage kt: A's blocks, then B's
+    auto read = [&](int slot, int kt, int kk, int f) {
+      if (f < kMI) fa[slot][f] = fragment<MA, BM>(sa(kt), wm + 32 * f, kk, lane);
+      else fb[slot][f - kMI] = fragment<kModeB, BN>(sb(kt), wn + 32 * (f - kMI), kk, lane);
+    };
+    constexpr int kFrags = kMI + kNI, kMfmas = kMI * kNI;
+#pragma unroll
+    for (int f = 0; f < kFrags; ++f) read(0, 0, 0, f);
+    // one step: its MFMAs, each followed by its share of the next step's reads
+    // (of stage kt1, step kk1) and, in the last step, of the copies of stage kt + 2
+    auto step = [&](int kt, int kk, int kt1, int kk1) {
+      const int cur = kk & 1, nxt = cur ^ 1;
+#pragma unroll
+      for (int m = 0; m < kMfmas; ++m) {
+        const int i = m / kNI, j = m % kNI;
+        if constexpr (FOLD > 0) acc[i][j] = mma(fa[cur][i], fb[cur][j], acc[i][j], T());
+        else out[i][j] = mma(fa[cur][i], fb[cur][j], out[i][j], T());
+#pragma unroll
+        for (int f = m * kFrags / kMfmas; f < (m + 1) * kFrags / kMfmas; ++f) read(nxt, kt1, kk1, f);
+        if (kk == 3) {
+#pragma unroll
+          for (int q = m * kCopies / kMfmas; q < (m + 1) * kCopies / kMfmas; ++q) copy(kt + 2, q);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    };
+    auto stage = [&](int kt) {
+      step(kt, 0, kt, 1);
+      step(kt, 1, kt, 2);
+      step(kt, 2, kt, 3);
+      wait_vmcnt<0>();
+      lds_barrier();
+      // (past the end the copies read nothing and put zeros into a buffer that
+      // is not read again: no branch cuts the block of code that `step` orders)
+      start(kt + 2);
+      if (kt + 2 < nk) write(kt + 2);
+      if (kt + 3 < nk) load(kt + 3);
+      __builtin_amdgcn_sched_barrier(0);
+      step(kt, 3, kt + 1, 0);
+    };
+    if constexpr (FOLD > 0) {
+      for (int k0 = 0; k0 < nk; k0 += FOLD) {
+        zero(acc);
+        const int k1 = min(k0 + FOLD, nk);
+#pragma unroll 1
+        for (int kt = k0; kt < k1; ++kt) stage(kt);
+#pragma unroll
+        for (int i = 0; i < kMI; ++i)
+#pragma unroll
+          for (int j = 0; j < kNI; ++j) out[i][j] += acc[i][j];
+      }
+    } else {
+#pragma unroll 1
+      for (int kt = 0; kt < nk; ++kt) stage(kt);
+    }
+    wait_vmcnt<0>();
   }
 };
 
@@ -388,7 +441,7 @@ struct RowProduct {
 };
 
 template <typename T, int MB, int BM, int BN, int WM, int WN, bool DMA>
-__global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void row_product_kernel(RowProduct g) {
+__global__ __launch_bounds__((BM / WM) * (BN / WN) * 64, BM * BN == 128 * 128 ? 2 : 1) void row_product_kernel(RowProduct g) {
   using K = Tile<T, kRows, MB, BM, BN, WM, WN, DMA>;
   constexpr int kStage = 32 * (WN + 8);         // elements of a wave's output staging
   static_assert(K::kWaves * kStage * 2 <= K::kLds, "staging fits");
@@ -468,7 +521,7 @@ struct WeightProduct {
 };
 
 template <typename T, int MB, int BM, int BN, int WM, int WN, bool DMA>
-__global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void weight_product_kernel(WeightProduct g) {
+__global__ __launch_bounds__((BM / WM) * (BN / WN) * 64, BM * BN == 128 * 128 ? 2 : 1) void weight_product_kernel(WeightProduct g) {
   using K = Tile<T, kCols, MB, BM, BN, WM, WN, DMA>;
   __shared__ __align__(16) char smem[K::kLds];
   const int per = g.tiles_m * g.tiles_n;
@@ -579,12 +632,13 @@ void row_product(const GroupArgs& x, int width, int depth, hipStream_t stream) {
   // copies straight to LDS need rows on 16 bytes, and a contraction in whole
   // chunks where an operand runs along it
   const bool dma = aligned16(x.a) && aligned16(x.b) && x.lda % 8 == 0 && x.ldb % 8 == 0 && x.b_stride % 8 == 0 && depth % 8 == 0;
-  run_rows<T, MB, 128, 128, 64, 64>(g, dma, stream);
+  if (x.rows / x.experts >= 192) run_rows<T, MB, 256, 256, 128, 128>(g, dma, stream);
+  else run_rows<T, MB, 128, 128, 64, 64>(g, dma, stream);
 }
 
 template <typename T, int MB>
 void weight_product(const GroupArgs& x, hipStream_t stream) {
-  constexpr int BM = 128, BN = 128;
+  constexpr int BM = 256, BN = 128, WM = 128, WN = 64;
   WeightProduct g;
   g.dy = x.a;
   g.x = x.b;
@@ -608,8 +662,8 @@ void weight_product(const GroupArgs& x, hipStream_t stream) {
   g.accumulate = split ? 0 : x.accumulate;
   const dim3 grid(unsigned(int64_t(g.tiles_m) * g.tiles_n * x.experts * x.splits));
   const bool dma = aligned16(x.a) && x.lda % 8 == 0 && (MB == kCodes || (aligned16(x.b) && x.ldb % 8 == 0));
-  if (dma) weight_product_kernel<T, MB, BM, BN, 64, 64, true><<<grid, 256, 0, stream>>>(g);
-  else weight_product_kernel<T, MB, BM, BN, 64, 64, false><<<grid, 256, 0, stream>>>(g);
+  if (dma) weight_product_kernel<T, MB, BM, BN, WM, WN, true><<<grid, 256, 0, stream>>>(g);
+  else weight_product_kernel<T, MB, BM, BN, WM, WN, false><<<grid, 256, 0, stream>>>(g);
   if (split) {
     const int blocks = (x.k + 1023) / 1024;
     weight_reduce_kernel<<<dim3(unsigned(int64_t(blocks) * x.n * x.experts)), 256, 0, stream>>>(
@@ -642,7 +696,7 @@ hipError_t launch_grouped_weight_grad(Elem t, const GroupArgs& g, hipStream_t st
 // least 1024 rows each on average (a partial costs 8 bytes of traffic an
 // element, 1024 rows of contraction about 40 times that in matrix time).
 int32_t weight_grad_splits(int64_t rows, int64_t experts, int64_t n, int64_t k, int cus) {
-  const int64_t tiles = ((n + 127) / 128) * ((k + 127) / 128) * experts;
+  const int64_t tiles = ((n + 255) / 256) * ((k + 127) / 128) * experts;
   const int64_t want = (2 * int64_t(cus) + tiles - 1) / tiles, most = rows / experts / 1024;
   const int64_t s = want < most ? want : most;
   return int32_t(s < 1 ? 1 : s);
