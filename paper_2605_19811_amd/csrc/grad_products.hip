@@ -17,6 +17,8 @@
 // Ragged edges cost no branch in the loop: operands are read by buffer loads
 // whose descriptor ends at the last valid row, so what lies beyond reads as zero,
 // and lanes beyond the end of the contraction get an address outside.
+#include <algorithm>
+
 #include "grad_device.h"
 
 namespace lm {
@@ -106,11 +108,28 @@ __device__ __forceinline__ bool find_tile(const int32_t* offsets, int experts, i
 
 enum { kRows = 0, kCols = 1, kCodes = 2 };   // operand: along, across, across in 8 bits
 
-// Workgroup `bid` of `n` as the number of a tile, such that the workgroups of an XCD
-// (every eighth) take neighbouring tiles, which share operands in its L2.
-__device__ __forceinline__ int by_xcd(int bid, int n) {
-  const int q = n / 8, r = n % 8, x = bid % 8;
-  return x * q + min(x, r) + bid / 8;
+// Workgroup `bid` as the number of a tile: an XCD (every eighth workgroup) takes
+// runs of `chunk` neighbouring tiles, as many as it runs at a time, which share
+// operands in its L2; the next run is another XCD's, so that each XCD gets
+// its part of every expert, the long ones too.
+__device__ __forceinline__ int by_xcd(int bid, int chunk) {
+  const int x = bid % 8, j = bid / 8;
+  return (j / chunk * 8 + x) * chunk + j % chunk;
+}
+
+// The nth longest expert (n-th in order where there are too many to sort on
+// the way): workgroups start in this order, so that no long one starts last.
+__device__ __forceinline__ int nth_longest(const int32_t* offsets, int experts, int rows, int n) {
+  if (experts == 1 || experts > 64) return n;
+  const int lane = threadIdx.x & 63, i = min(lane, experts - 1);
+  const int len = lane < experts ? min(max(offsets[i + 1], 0), rows) - min(max(offsets[i], 0), rows) : INT32_MIN;
+  int rank = 0;
+  for (int j = 0; j < experts; ++j) {
+    const int other = __builtin_amdgcn_readlane(len, j);
+    rank += other > len || (other == len && j < lane) ? 1 : 0;
+  }
+  const uint64_t m = __ballot(lane < experts && rank == n);
+  return __builtin_amdgcn_readfirstlane(63 - __builtin_clzll(m | 1));
 }
 
 // Tile `id` of m x n as (row, column), in bands of eight rows: the tiles that run
@@ -148,14 +167,15 @@ struct Source {
   int rows;             // kRows: rows of the tile that exist
   int cols;             // kCols: columns of the matrix from the tile's first on
   int depth;            // contraction values
+  bool wide;            // the matrix's rows hold at least eight elements
 };
 
-template <typename T, int MA, int MB, int BM, int BN, int WM, int WN, bool DMA>
+template <typename T, int MA, int MB, int BM, int BN, int WM, int WN, int NB, bool DMA>
 struct Tile {
   static constexpr int kWavesN = BN / WN, kWaves = (BM / WM) * kWavesN, kThreads = kWaves * 64;
   static constexpr int kMI = WM / 32, kNI = WN / 32;
   static constexpr int kStageBytes = (BM + BN) * 128;
-  static constexpr int kLds = 2 * kStageBytes;
+  static constexpr int kLds = NB * kStageBytes;      // NB stages
   using SA = Stage<MA, BM>;
   using SB = Stage<MB, BN>;
 
@@ -194,41 +214,72 @@ struct Tile {
     }
   };
 
-  // The same through registers, for rows off 16 bytes: a chunk that reaches over
-  // the end of its row goes element by element.
+  // The same through registers, for rows off 16 bytes. Chunks are loaded 16 bytes at
+  // a time from wherever they start; one that reaches over the end of its row is
+  // loaded from where it ends there and shifted into place on its way into
+  // LDS, so that no load waits in a branch of its own.
   template <int MODE, int W>
   struct Regs {
     static constexpr int kInst = Stage<MODE, W>::kChunks / kThreads;
     u32x4 v[kInst];
   };
+  // Elements of chunk q of a thread that exist (at most 8; 0: none).
+  template <int MODE, int W>
+  __device__ static __forceinline__ int present(const Source& s, int k0, int q, int tid, int* row, int* first) {
+    int chunk;
+    Stage<MODE, W>::place(q * kThreads + tid, row, &chunk);
+    *first = chunk * 8;
+    const int n = (MODE == kRows ? s.depth - k0 : s.cols) - *first;
+    const bool in = *row < (MODE == kRows ? s.rows : s.depth - k0);
+    return in ? max(min(n, 8), 0) : 0;
+  }
   template <int MODE, int W>
   __device__ static __forceinline__ void fetch(const Source& s, int k0, int tid, Regs<MODE, W>& r) {
-    using S = Stage<MODE, W>;
+    const char* base = s.p + (MODE == kRows ? int64_t(k0) * 2 : int64_t(k0) * s.ld);
+    const int left = MODE == kRows ? s.depth - k0 : s.cols;    // of the first row
+    if (s.wide) {
+      const int safe = left < 8 ? left * 2 : 16;               // its first chunk
 #pragma unroll
-    for (int q = 0; q < Regs<MODE, W>::kInst; ++q) {
-      int row, chunk;
-      S::place(q * kThreads + tid, &row, &chunk);
-      const int first = MODE == kRows ? k0 + chunk * 8 : chunk * 8;
-      const int n = (MODE == kRows ? s.depth : s.cols) - first;
-      const bool in = MODE == kRows ? row < s.rows : k0 + row < s.depth;
-      u32x4 v = {0u, 0u, 0u, 0u};
-      if (in && n > 0) {
-        const uint16_t* p = reinterpret_cast<const uint16_t*>(s.p + int64_t(MODE == kRows ? row : k0 + row) * s.ld) + first;
-        if (n >= 8) {
-          __builtin_memcpy(&v, p, 16);
-        } else {
-#pragma unroll
-          for (int j = 0; j < 8; ++j)
-            if (j < n) v[j >> 1] |= uint32_t(p[j]) << (16 * (j & 1));
-        }
+      for (int q = 0; q < Regs<MODE, W>::kInst; ++q) {
+        int row, first;
+        const int n = present<MODE, W>(s, k0, q, tid, &row, &first);
+        const uint32_t off = n > 0 ? uint32_t(row) * uint32_t(s.ld) + uint32_t(first * 2 + n * 2) : uint32_t(safe);
+        __builtin_memcpy(&r.v[q], (base - 16) + off, 16);
       }
-      r.v[q] = v;
+    } else {
+#pragma unroll
+      for (int q = 0; q < Regs<MODE, W>::kInst; ++q) {
+        int row, first;
+        const int n = present<MODE, W>(s, k0, q, tid, &row, &first);
+        const uint16_t* p = reinterpret_cast<const uint16_t*>(base + (n > 0 ? int64_t(row) * s.ld + first * 2 : 0));
+        u32x4 v = {0u, 0u, 0u, 0u};
+        for (int j = 0; j < n; ++j) {                          // in the high end, as above
+          v[0] = (v[0] >> 16) | (v[1] << 16);
+          v[1] = (v[1] >> 16) | (v[2] << 16);
+          v[2] = (v[2] >> 16) | (v[3] << 16);
+          v[3] = (v[3] >> 16) | (uint32_t(p[j]) << 16);
+        }
+        r.v[q] = v;
+      }
     }
   }
   template <int MODE, int W>
-  __device__ static __forceinline__ void put(const Regs<MODE, W>& r, char* dst, int tid) {
+  __device__ static __forceinline__ void put(const Source& s, int k0, const Regs<MODE, W>& r, char* dst, int tid) {
+    const bool cut = MODE == kRows ? s.depth - k0 < 64 && s.depth % 8 != 0 : s.cols < W && s.cols % 8 != 0;
 #pragma unroll
-    for (int q = 0; q < Regs<MODE, W>::kInst; ++q) *reinterpret_cast<u32x4*>(dst + (q * kThreads + tid) * 16) = r.v[q];
+    for (int q = 0; q < Regs<MODE, W>::kInst; ++q) {
+      int row, first;
+      const int n = present<MODE, W>(s, k0, q, tid, &row, &first);
+      u32x4 v = r.v[q];
+      if (cut) {      // (uniform) down by 8 - n elements
+        const int by = 8 - n;
+        if (by & 1) v = u32x4{(v[0] >> 16) | (v[1] << 16), (v[1] >> 16) | (v[2] << 16), (v[2] >> 16) | (v[3] << 16), v[3] >> 16};
+        if (by & 2) v = u32x4{v[1], v[2], v[3], 0u};
+        if (by & 4) v = u32x4{v[2], v[3], 0u, 0u};
+      }
+      if (n <= 0) v = u32x4{0u, 0u, 0u, 0u};
+      *reinterpret_cast<u32x4*>(dst + (q * kThreads + tid) * 16) = v;
+    }
   }
 
   // A checkpoint's stage: 16 codes a load, widened to bf16 (exactly: the scale
@@ -250,7 +301,7 @@ struct Tile {
     for (int q = 0; q < CodeRegs::kInst; ++q) {
       const int i = q * kThreads + tid, row = i / kPer, c = (i % kPer) * 16;
       const bool in = k0 + row < s.depth && c < s.cols;
-      const int64_t at = in ? k0 + row : 0;
+      const int64_t at = in ? k0 + row : 0;      // (past the end: any row)
       const int col = in ? c : 0;
       const u32x4 v = *reinterpret_cast<const u32x4*>(s.codes + at * s.ld + col);
       const uint32_t e = s.scales[at * s.lds + col / kCkptBlock];
@@ -258,23 +309,19 @@ struct Tile {
       r.s[q] = in ? e : 127u;
     }
   }
-  __device__ static __forceinline__ void put(const CodeRegs& r, char* dst, int tid) {
+  static constexpr int kPieces = 2 * CodeRegs::kInst;           // of eight values a thread
+  __device__ static __forceinline__ void put(const CodeRegs& r, int piece, char* dst, int tid) {
     constexpr int kPer = BN / 16;
+    const int q = piece >> 1, h = piece & 1;
+    const int i = q * kThreads + tid, row = i / kPer, c = (i % kPer) * 2 + h;   // logical chunk
+    const float scale = scale_of(r.s[q]);
+    u32x4 o;
 #pragma unroll
-    for (int q = 0; q < CodeRegs::kInst; ++q) {
-      const int i = q * kThreads + tid, row = i / kPer, c = (i % kPer) * 2;   // logical chunk
-      const float scale = scale_of(r.s[q]);
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        u32x4 o;
-#pragma unroll
-        for (int w = 0; w < 2; ++w) {
-          o[2 * w] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(r.v[q][2 * h + w], scale, false));
-          o[2 * w + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(r.v[q][2 * h + w], scale, true));
-        }
-        *reinterpret_cast<u32x4*>(dst + row * (BN * 2) + ((c + h) ^ SB::swz(row)) * 16) = o;
-      }
+    for (int w = 0; w < 2; ++w) {
+      o[2 * w] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(r.v[q][2 * h + w], scale, false));
+      o[2 * w + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(r.v[q][2 * h + w], scale, true));
     }
+    *reinterpret_cast<u32x4*>(dst + row * (BN * 2) + (c ^ SB::swz(row)) * 16) = o;
   }
 
   // Fragment of 32 rows (or columns) from `w0` on and contraction values
@@ -306,21 +353,22 @@ struct Tile {
   //
   // A stage is four steps of 16 values. The fragments of a step are read while the
   // step before is multiplied, across stages too: one barrier a stage, before its
-  // last step, says that every wave has read the stage (its buffer takes the stage after
-  // the next) and that the next one has landed. Copies and fragment reads are
-  // placed one behind each MFMA, so that the matrix unit never waits for a batch of them.
+  // last step, says that every wave has read the stage (its buffer takes the stage NB
+  // later) and that the next one has landed. Copies and fragment reads are
+  // placed one behind each MFMA, so that the matrix unit never waits for a batch of
+  // them, and so are the codes' conversions.
   template <int FOLD>
   __device__ static __forceinline__ void product(const Source& a, const Source& b, const CodeSource& c, int depth, char* smem, f32x16 (&out)[kMI][kNI]) {
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wm = (wave / kWavesN) * WM, wn = (wave % kWavesN) * WN;
     const int nk = (depth + 63) / 64;
-    auto sa = [&](int kt) { return smem + (kt & 1) * kStageBytes; };
-    auto sb = [&](int kt) { return smem + (kt & 1) * kStageBytes + BM * 128; };
     constexpr int kModeB = MB == kCodes ? int(kCols) : MB;
     constexpr bool kDmaB = DMA && MB != kCodes;
     constexpr int kCopiesA = DMA ? Copier<MA, BM>::kInst : 0, kCopiesB = kDmaB ? Copier<kModeB, BN>::kInst : 0;
     constexpr int kCopies = kCopiesA + kCopiesB;
+    constexpr int kPiecesB = MB == kCodes ? kPieces : 0;
+    constexpr int kCodeLoads = MB == kCodes ? 2 * CodeRegs::kInst : 0;
     Copier<MA, BM> ca(a, wave, lane);
     Copier<kModeB, BN> cb(b, wave, lane);
     Regs<MA, DMA ? 0 : BM> ra;
@@ -329,21 +377,23 @@ struct Tile {
     // stages that go through registers: loaded one stage ahead of the write to LDS
     auto load = [&](int kt) {
       if constexpr (!DMA) fetch<MA, BM>(a, kt * 64, tid, ra);
+      if constexpr (!DMA && MB != kCodes) fetch<kModeB, BN>(b, kt * 64, tid, rb);
+    };
+    auto load_codes = [&](int kt) {
       if constexpr (MB == kCodes) fetch(c, kt * 64, tid, rc);
-      else if constexpr (!DMA) fetch<kModeB, BN>(b, kt * 64, tid, rb);
     };
-    auto write = [&](int kt) {
-      if constexpr (!DMA) put<MA, BM>(ra, sa(kt), tid);
-      if constexpr (MB == kCodes) put(rc, sb(kt), tid);
-      else if constexpr (!DMA) put<kModeB, BN>(rb, sb(kt), tid);
+    auto write = [&](int kt, char* buf) {
+      if constexpr (!DMA) put<MA, BM>(a, kt * 64, ra, buf, tid);
+      if constexpr (!DMA && MB != kCodes) put<kModeB, BN>(b, kt * 64, rb, buf + BM * 128, tid);
     };
+    auto widen = [&](int piece, char* buf) { put(rc, piece, buf + BM * 128, tid); };
     auto start = [&](int kt) {
       if constexpr (DMA) ca.start(kt * 64);
       if constexpr (kDmaB) cb.start(kt * 64);
     };
-    auto copy = [&](int kt, int q) {
-      if (q < kCopiesA) ca.copy(q, sa(kt), wave);
-      else cb.copy(q - kCopiesA, sb(kt), wave);
+    auto copy = [&](int q, char* buf) {
+      if (q < kCopiesA) ca.copy(q, buf, wave);
+      else cb.copy(q - kCopiesA, buf + BM * 128, wave);
     };
     f32x16 acc[FOLD ? kMI : 1][FOLD ? kNI : 1];
     auto zero = [](auto& x) {
@@ -352,31 +402,39 @@ struct Tile {
     };
     zero(out);
     if (nk == 0) return;
+    // (past the end copies read nothing and put zeros into a buffer that is not
+    // read again: the number of copies in flight is always the same, and no
+    // branch cuts the block of code that `step` orders)
 #pragma unroll
-    for (int kt = 0; kt < 2; ++kt) {
+    for (int kt = 0; kt < NB; ++kt) {
+      char* buf = smem + kt * kStageBytes;
+      start(kt);
+#pragma unroll
+      for (int q = 0; q < kCopies; ++q) copy(q, buf);
       if (kt < nk) {
-        start(kt);
-#pragma unroll
-        for (int q = 0; q < kCopies; ++q) copy(kt, q);
         load(kt);
-        write(kt);
+        write(kt, buf);
       }
+      load_codes(kt);
+#pragma unroll
+      for (int h = 0; h < kPiecesB; ++h) widen(h, buf);
     }
-    if (2 < nk) load(2);
-    wait_vmcnt<0>();
+    if (NB < nk) load(NB);
+    load_codes(NB);
+    if constexpr (DMA) wait_vmcnt<0>();
     lds_barrier();
     s16x8 fa[2][kMI], fb[2][kNI];
-    // fragment f of step kk (0..3) of stage kt: A's blocks, then B's
-    auto read = [&](int slot, int kt, int kk, int f) {
-      if (f < kMI) fa[slot][f] = fragment<MA, BM>(sa(kt), wm + 32 * f, kk, lane);
-      else fb[slot][f - kMI] = fragment<kModeB, BN>(sb(kt), wn + 32 * (f - kMI), kk, lane);
+    // fragment f of step kk (0..3) of the stage in `buf`: A's blocks, then B's
+    auto read = [&](int slot, const char* buf, int kk, int f) {
+      if (f < kMI) fa[slot][f] = fragment<MA, BM>(buf, wm + 32 * f, kk, lane);
+      else fb[slot][f - kMI] = fragment<kModeB, BN>(buf + BM * 128, wn + 32 * (f - kMI), kk, lane);
     };
     constexpr int kFrags = kMI + kNI, kMfmas = kMI * kNI;
 #pragma unroll
-    for (int f = 0; f < kFrags; ++f) read(0, 0, 0, f);
-    // one step: its MFMAs, each followed by its share of the next step's reads
-    // (of stage kt1, step kk1) and, in the last step, of the copies of stage kt + 2
-    auto step = [&](int kt, int kk, int kt1, int kk1) {
+    for (int f = 0; f < kFrags; ++f) read(0, smem, 0, f);
+    // one step: its MFMAs, each followed by its share of the next step's reads (step
+    // kk1 of the stage in `next`) and, in the last step, of what fills `fill`
+    auto step = [&](int kk, const char* next, int kk1, char* fill) {
       const int cur = kk & 1, nxt = cur ^ 1;
 #pragma unroll
       for (int m = 0; m < kMfmas; ++m) {
@@ -384,27 +442,34 @@ struct Tile {
         if constexpr (FOLD > 0) acc[i][j] = mma(fa[cur][i], fb[cur][j], acc[i][j], T());
         else out[i][j] = mma(fa[cur][i], fb[cur][j], out[i][j], T());
 #pragma unroll
-        for (int f = m * kFrags / kMfmas; f < (m + 1) * kFrags / kMfmas; ++f) read(nxt, kt1, kk1, f);
+        for (int f = m * kFrags / kMfmas; f < (m + 1) * kFrags / kMfmas; ++f) read(nxt, next, kk1, f);
         if (kk == 3) {
 #pragma unroll
-          for (int q = m * kCopies / kMfmas; q < (m + 1) * kCopies / kMfmas; ++q) copy(kt + 2, q);
+          for (int q = m * kCopies / kMfmas; q < (m + 1) * kCopies / kMfmas; ++q) copy(q, fill);
+#pragma unroll
+          for (int h = m * kPiecesB / kMfmas; h < (m + 1) * kPiecesB / kMfmas; ++h) widen(h, fill);
         }
         __builtin_amdgcn_sched_barrier(0);
       }
     };
+    char* buf = smem;
     auto stage = [&](int kt) {
-      step(kt, 0, kt, 1);
-      step(kt, 1, kt, 2);
-      step(kt, 2, kt, 3);
-      wait_vmcnt<0>();
+      char* next = buf == smem + (NB - 1) * kStageBytes ? smem : buf + kStageBytes;
+      step(0, buf, 1, buf);
+      step(1, buf, 2, buf);
+      step(2, buf, 3, buf);
+      // stage kt + 1 has landed: only copies of later ones, and the codes
+      // loaded after them, are still on their way
+      if constexpr (DMA) wait_vmcnt<(NB - 2) * (kCopies + kCodeLoads) + kCodeLoads>();
       lds_barrier();
-      // (past the end the copies read nothing and put zeros into a buffer that
-      // is not read again: no branch cuts the block of code that `step` orders)
-      start(kt + 2);
-      if (kt + 2 < nk) write(kt + 2);
-      if (kt + 3 < nk) load(kt + 3);
+      start(kt + NB);
+      if (kt + NB < nk) write(kt + NB, buf);
+      if (kt + NB + 1 < nk) load(kt + NB + 1);
       __builtin_amdgcn_sched_barrier(0);
-      step(kt, 3, kt + 1, 0);
+      step(3, next, 0, buf);
+      load_codes(kt + NB + 1);       // (their registers are free now)
+      __builtin_amdgcn_sched_barrier(0);
+      buf = next;
     };
     if constexpr (FOLD > 0) {
       for (int k0 = 0; k0 < nk; k0 += FOLD) {
@@ -436,18 +501,20 @@ struct RowProduct {
   int64_t lda, ldb, ldc, b_stride;    // elements
   int rows, experts;
   int width, depth;                   // columns of the output, contraction
-  int slots, tiles_n;
+  int slots, tiles_n, chunk;
   int vec_out;                        // rows of the output start 16-byte aligned
 };
 
-template <typename T, int MB, int BM, int BN, int WM, int WN, bool DMA>
+template <typename T, int MB, int BM, int BN, int WM, int WN, int NB, bool DMA>
 __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64, BM * BN == 128 * 128 ? 2 : 1) void row_product_kernel(RowProduct g) {
-  using K = Tile<T, kRows, MB, BM, BN, WM, WN, DMA>;
+  using K = Tile<T, kRows, MB, BM, BN, WM, WN, NB, DMA>;
   constexpr int kStage = 32 * (WN + 8);         // elements of a wave's output staging
   static_assert(K::kWaves * kStage * 2 <= K::kLds, "staging fits");
   __shared__ __align__(16) char smem[K::kLds];
   int slot, tn;
-  banded(by_xcd(blockIdx.x, gridDim.x), g.slots, g.tiles_n, &slot, &tn);
+  const int id = by_xcd(blockIdx.x, g.chunk);
+  if (id >= g.slots * g.tiles_n) return;
+  banded(id, g.slots, g.tiles_n, &slot, &tn);
   RowTile t;
   if (!find_tile<BM>(g.offsets, g.experts, g.rows, slot, &t)) return;
   const int col0 = tn * BN;
@@ -458,11 +525,13 @@ __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64, BM * BN == 128 * 128 ? 
   a.rows = min(t.end - t.row0, BM);
   a.depth = g.depth;
   a.cols = 0;
+  a.wide = g.depth >= 8;
   b.p = reinterpret_cast<const char*>(MB == kRows ? w + col0 * g.ldb : w + col0);
   b.ld = g.ldb * 2;
   b.rows = min(g.width - col0, BN);
   b.cols = g.width - col0;
   b.depth = g.depth;
+  b.wide = (MB == kRows ? g.depth : g.width) >= 8;
   f32x16 acc[K::kMI][K::kNI];
   K::template product<0>(a, b, typename K::CodeSource{}, g.depth, smem, acc);
   lds_barrier();
@@ -516,20 +585,21 @@ struct WeightProduct {
   int64_t lddy, ldx, ldo, o_stride;   // elements; o_stride: of an expert
   int64_t split_stride;               // partials: of a split
   int rows, experts, n, k;
-  int tiles_m, tiles_n, splits;
+  int tiles_m, tiles_n, splits, chunk;
   int accumulate;
 };
 
-template <typename T, int MB, int BM, int BN, int WM, int WN, bool DMA>
+template <typename T, int MB, int BM, int BN, int WM, int WN, int NB, bool DMA>
 __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64, BM * BN == 128 * 128 ? 2 : 1) void weight_product_kernel(WeightProduct g) {
-  using K = Tile<T, kCols, MB, BM, BN, WM, WN, DMA>;
+  using K = Tile<T, kCols, MB, BM, BN, WM, WN, NB, DMA>;
   __shared__ __align__(16) char smem[K::kLds];
   const int per = g.tiles_m * g.tiles_n;
-  int id = by_xcd(blockIdx.x, gridDim.x);
-  const int unit = id / per;
+  const int id = by_xcd(blockIdx.x, g.chunk), unit = id / per;
+  if (unit >= g.experts * g.splits) return;
   int tm, tn;
   banded(id - unit * per, g.tiles_m, g.tiles_n, &tm, &tn);
-  const int e = unit / g.splits, s = unit - e * g.splits;
+  const int nth = unit / g.splits, s = unit - nth * g.splits;
+  const int e = nth_longest(g.offsets, g.experts, g.rows, nth);
   const int first = min(max(g.offsets[e], 0), g.rows), end = min(max(g.offsets[e + 1], 0), g.rows);
   // this split's rows: whole stages, the same number for every split
   const int len = max(end - first, 0);
@@ -544,6 +614,7 @@ __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64, BM * BN == 128 * 128 ? 
   a.rows = 0;
   a.cols = g.n - m0;
   a.depth = depth;
+  a.wide = g.n >= 8;
   if constexpr (MB == kCodes) {
     c.codes = g.kept.codes + row0 * g.kept.ld_codes + n0;
     c.scales = g.kept.scales + row0 * g.kept.ld_scales + n0 / kCkptBlock;
@@ -557,6 +628,7 @@ __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64, BM * BN == 128 * 128 ? 
     b.rows = 0;
     b.cols = g.k - n0;
     b.depth = depth;
+    b.wide = g.k >= 8;
   }
   f32x16 acc[K::kMI][K::kNI];
   K::template product<4>(a, b, c, depth, smem, acc);
@@ -603,14 +675,20 @@ __global__ __launch_bounds__(256) void weight_reduce_kernel(const float* partial
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 
-template <typename T, int MB, int BM, int BN, int WM, int WN>
+// Grid of `tiles` tiles in runs of `chunk`, a multiple of eight of them.
+unsigned grid_of(int64_t tiles, int64_t chunk) { return unsigned((tiles + 8 * chunk - 1) / (8 * chunk) * 8 * chunk); }
+
+template <typename T, int MB, int BM, int BN, int WM, int WN, int NB>
 void run_rows(RowProduct g, bool dma, hipStream_t stream) {
   g.slots = g.rows / BM + g.experts;
   g.tiles_n = (g.width + BN - 1) / BN;
-  const dim3 grid(unsigned(int64_t(g.slots) * g.tiles_n));
+  // one run an XCD: tiles cost the same
+  const int64_t tiles = int64_t(g.slots) * g.tiles_n;
+  g.chunk = int((tiles + 7) / 8);
+  const dim3 grid(grid_of(tiles, g.chunk));
   constexpr int kThreads = (BM / WM) * (BN / WN) * 64;
-  if (dma) row_product_kernel<T, MB, BM, BN, WM, WN, true><<<grid, kThreads, 0, stream>>>(g);
-  else row_product_kernel<T, MB, BM, BN, WM, WN, false><<<grid, kThreads, 0, stream>>>(g);
+  if (dma) row_product_kernel<T, MB, BM, BN, WM, WN, NB, true><<<grid, kThreads, 0, stream>>>(g);
+  else row_product_kernel<T, MB, BM, BN, WM, WN, NB, false><<<grid, kThreads, 0, stream>>>(g);
 }
 
 template <typename T, int MB>
@@ -632,13 +710,13 @@ void row_product(const GroupArgs& x, int width, int depth, hipStream_t stream) {
   // copies straight to LDS need rows on 16 bytes, and a contraction in whole
   // chunks where an operand runs along it
   const bool dma = aligned16(x.a) && aligned16(x.b) && x.lda % 8 == 0 && x.ldb % 8 == 0 && x.b_stride % 8 == 0 && depth % 8 == 0;
-  if (x.rows / x.experts >= 192) run_rows<T, MB, 256, 256, 128, 128>(g, dma, stream);
-  else run_rows<T, MB, 128, 128, 64, 64>(g, dma, stream);
+  if (x.rows / x.experts >= 192) run_rows<T, MB, 256, 256, 128, 128, 2>(g, dma, stream);
+  else run_rows<T, MB, 128, 128, 64, 64, 2>(g, dma, stream);
 }
 
 template <typename T, int MB>
 void weight_product(const GroupArgs& x, hipStream_t stream) {
-  constexpr int BM = 256, BN = 128, WM = 128, WN = 64;
+  constexpr int BM = 256, BN = 128, WM = 128, WN = 64, NB = 3;
   WeightProduct g;
   g.dy = x.a;
   g.x = x.b;
@@ -660,10 +738,13 @@ void weight_product(const GroupArgs& x, hipStream_t stream) {
   g.o_stride = split ? one : x.c_stride;
   g.split_stride = split ? one * x.experts : 0;
   g.accumulate = split ? 0 : x.accumulate;
-  const dim3 grid(unsigned(int64_t(g.tiles_m) * g.tiles_n * x.experts * x.splits));
+  // an expert's tiles over all XCDs: those of one expert cost the same
+  const int64_t per = int64_t(g.tiles_m) * g.tiles_n;
+  g.chunk = int((per + 7) / 8);
+  const dim3 grid(grid_of(per * x.experts * x.splits, g.chunk));
   const bool dma = aligned16(x.a) && x.lda % 8 == 0 && (MB == kCodes || (aligned16(x.b) && x.ldb % 8 == 0));
-  if (dma) weight_product_kernel<T, MB, BM, BN, WM, WN, true><<<grid, 256, 0, stream>>>(g);
-  else weight_product_kernel<T, MB, BM, BN, WM, WN, false><<<grid, 256, 0, stream>>>(g);
+  if (dma) weight_product_kernel<T, MB, BM, BN, WM, WN, NB, true><<<grid, 256, 0, stream>>>(g);
+  else weight_product_kernel<T, MB, BM, BN, WM, WN, NB, false><<<grid, 256, 0, stream>>>(g);
   if (split) {
     const int blocks = (x.k + 1023) / 1024;
     weight_reduce_kernel<<<dim3(unsigned(int64_t(blocks) * x.n * x.experts)), 256, 0, stream>>>(
