@@ -10,6 +10,7 @@ import os
 import shutil
 import subprocess
 import sys
+from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
@@ -20,6 +21,8 @@ LIB = os.path.join(HERE, "liblionmuon.so")
 ROCM = os.environ.get("ROCM_PATH", "/opt/rocm")
 HIPCC = os.path.join(ROCM, "bin", "hipcc")
 ARCH = "gfx950"
+SOURCES = ("grad_products.hip", "kernels.hip", "scratch.hip", "grad_rows.hip", "plan.cpp",
+           "api.cpp", "grad_api.cpp")
 
 # Packed-fp32 VALU forms are kept out of the device code (the host pass warns
 # that it does not know the feature; that is harmless).
@@ -46,16 +49,16 @@ def _run(cmd, verbose):
 def build(verbose: bool = False) -> str:
     os.makedirs(BUILD, exist_ok=True)
     inc = [f"-I{INCLUDE}", f"-I{CSRC}"]
-    objs = []
-    for src in ("kernels.hip", "scratch.hip", "grad_rows.hip", "grad_products.hip"):
-        obj = os.path.join(BUILD, src + ".o")
-        _run([HIPCC, *HIP_FLAGS, *inc, "-c", os.path.join(CSRC, src), "-o", obj], verbose)
-        objs.append(obj)
     cxx = shutil.which("g++") or "g++"
-    for src in ("plan.cpp", "api.cpp", "grad_api.cpp"):
+
+    def compile_one(src):
         obj = os.path.join(BUILD, src + ".o")
-        _run([cxx, *CXX_FLAGS, *inc, "-c", os.path.join(CSRC, src), "-o", obj], verbose)
-        objs.append(obj)
+        tool = [HIPCC, *HIP_FLAGS] if src.endswith(".hip") else [cxx, *CXX_FLAGS]
+        _run([*tool, *inc, "-c", os.path.join(CSRC, src), "-o", obj], verbose)
+        return obj
+
+    with ThreadPoolExecutor(max_workers=len(SOURCES)) as pool:
+        objs = list(pool.map(compile_one, SOURCES))
     tmp = LIB + ".tmp"
     _run([HIPCC, "-shared", "-fPIC", f"--offload-arch={ARCH}", *objs, "-o", tmp,
           f"-L{ROCM}/lib", "-lamdhip64", f"-Wl,-rpath,{ROCM}/lib", "-Wl,--no-undefined"], verbose)

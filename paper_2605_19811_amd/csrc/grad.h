@@ -68,14 +68,14 @@ struct GroupArgs {
   int64_t rows = 0;
   int32_t experts = 0, n = 0, k = 0;
   int32_t accumulate = 0;
-  int32_t splits = 1;               // weight gradient: row ranges of an expert
-  float* partial = nullptr;         // splits x experts x n x k when splits > 1
+  float* partial = nullptr;         // weight gradient: weight_grad_partials() x n x k
   int32_t cus = 256;
 };
 hipError_t launch_grouped_product(Elem t, const GroupArgs& g, hipStream_t stream);
 hipError_t launch_grouped_input_grad(Elem t, const GroupArgs& g, hipStream_t stream);
 hipError_t launch_grouped_weight_grad(Elem t, const GroupArgs& g, hipStream_t stream);
-// Row ranges that the weight gradient is split into.
-int32_t weight_grad_splits(int64_t rows, int64_t experts, int64_t n, int64_t k, int cus);
+// Partial sums (n x k fp32 each) that the weight gradient of these sizes needs
+// room for: long experts are cut into parts where whole ones would leave CUs idle.
+int64_t weight_grad_partials(int64_t rows, int64_t experts, int64_t n, int64_t k, int cus);
 
 }  // namespace lm

@@ -32,58 +32,60 @@ struct Bad {
   lm_status status;
   std::string msg;
 };
-void need(bool ok, const std::string& msg) {
-  if (!ok) throw Bad{LM_ERR_INVALID_ARGUMENT, msg};
+[[noreturn]] void refuse(const char* name, const char* msg) {
+  throw Bad{LM_ERR_INVALID_ARGUMENT, *name ? std::string(name) + ": " + msg : std::string(msg)};
 }
+// (the message is put together for a refusal only)
+inline void need(bool ok, const char* name, const char* msg) {
+  if (!ok) refuse(name, msg);
+}
+inline void need(bool ok, const char* msg) { need(ok, "", msg); }
 
 size_t elem_bytes(int32_t dtype) { return dtype == LM_F32 ? 4 : 2; }
 
 void check_shape(const char* name, int64_t rows, int64_t cols, int64_t ld, int32_t dtype, uint32_t reserved) {
-  const std::string n(name);
-  need(dtype == LM_F32 || dtype == LM_BF16 || dtype == LM_F16, n + ": unknown dtype");
-  need(reserved == 0, n + ": reserved must be 0");
-  need(rows >= 0 && cols >= 0, n + ": negative size");
-  need(rows <= kMaxRows, n + ": too many rows");
-  need(ld >= cols, n + ": ld must be at least cols");
-  need(ld < kMaxLd, n + ": rows must be less than 2^22 elements apart");
+  need(dtype == LM_F32 || dtype == LM_BF16 || dtype == LM_F16, name, "unknown dtype");
+  need(reserved == 0, name, "reserved must be 0");
+  need(rows >= 0 && cols >= 0, name, "negative size");
+  need(rows <= kMaxRows, name, "too many rows");
+  need(ld >= cols, name, "ld must be at least cols");
+  need(ld < kMaxLd, name, "rows must be less than 2^22 elements apart");
 }
 
 void check(const char* name, const lm_matrix* m) {
-  need(m != nullptr, std::string(name) + ": null descriptor");
+  need(m != nullptr, name, "null descriptor");
   check_shape(name, m->rows, m->cols, m->ld, m->dtype, m->reserved);
   if (m->rows == 0 || m->cols == 0) return;
-  need(m->data != nullptr, std::string(name) + ": null data");
-  need(reinterpret_cast<uintptr_t>(m->data) % elem_bytes(m->dtype) == 0, std::string(name) + ": misaligned data");
+  need(m->data != nullptr, name, "null data");
+  need(reinterpret_cast<uintptr_t>(m->data) % elem_bytes(m->dtype) == 0, name, "misaligned data");
 }
 
 void check(const char* name, const lm_stack* m) {
-  const std::string n(name);
-  need(m != nullptr, n + ": null descriptor");
+  need(m != nullptr, name, "null descriptor");
   check_shape(name, m->rows, m->cols, m->ld, m->dtype, m->reserved);
-  need(m->count >= 0 && m->count <= kMaxRows, n + ": bad count");
+  need(m->count >= 0 && m->count <= kMaxRows, name, "bad count");
   if (m->count == 0 || m->rows == 0 || m->cols == 0) return;
-  need(m->data != nullptr, n + ": null data");
-  need(reinterpret_cast<uintptr_t>(m->data) % elem_bytes(m->dtype) == 0, n + ": misaligned data");
-  need(m->count == 1 || m->stride >= (m->rows - 1) * m->ld + m->cols, n + ": stride smaller than a matrix");
-  need(m->count == 1 || m->stride <= (int64_t(1) << 62) / (m->count * 4), n + ": stride too large");
+  need(m->data != nullptr, name, "null data");
+  need(reinterpret_cast<uintptr_t>(m->data) % elem_bytes(m->dtype) == 0, name, "misaligned data");
+  need(m->count == 1 || m->stride >= (m->rows - 1) * m->ld + m->cols, name, "stride smaller than a matrix");
+  need(m->count == 1 || m->stride <= (int64_t(1) << 62) / (m->count * 4), name, "stride too large");
 }
 
 void check(const char* name, const lm_checkpoint* c) {
-  const std::string n(name);
-  need(c != nullptr, n + ": null descriptor");
-  need(c->rows >= 0 && c->cols >= 0, n + ": negative size");
-  need(c->rows <= kMaxRows, n + ": too many rows");
-  need(c->ld_codes >= c->cols && c->ld_codes % 16 == 0, n + ": ld_codes must be a multiple of 16 and at least cols");
-  need(c->ld_codes <= kMaxLd, n + ": rows must be at most 2^22 bytes apart");
-  need(c->ld_scales >= (c->cols + LM_CHECKPOINT_BLOCK - 1) / LM_CHECKPOINT_BLOCK, n + ": ld_scales smaller than a row of scales");
-  need(c->ld_scales <= kMaxLd, n + ": rows of scales must be at most 2^22 bytes apart");
+  need(c != nullptr, name, "null descriptor");
+  need(c->rows >= 0 && c->cols >= 0, name, "negative size");
+  need(c->rows <= kMaxRows, name, "too many rows");
+  need(c->ld_codes >= c->cols && c->ld_codes % 16 == 0, name, "ld_codes must be a multiple of 16 and at least cols");
+  need(c->ld_codes <= kMaxLd, name, "rows must be at most 2^22 bytes apart");
+  need(c->ld_scales >= (c->cols + LM_CHECKPOINT_BLOCK - 1) / LM_CHECKPOINT_BLOCK, name, "ld_scales smaller than a row of scales");
+  need(c->ld_scales <= kMaxLd, name, "rows of scales must be at most 2^22 bytes apart");
   if (c->rows == 0 || c->cols == 0) return;
-  need(c->codes != nullptr && c->scales != nullptr, n + ": null data");
-  need(reinterpret_cast<uintptr_t>(c->codes) % 16 == 0, n + ": codes must be 16-byte aligned");
+  need(c->codes != nullptr && c->scales != nullptr, name, "null data");
+  need(reinterpret_cast<uintptr_t>(c->codes) % 16 == 0, name, "codes must be 16-byte aligned");
 }
 
 void same_shape(const char* what, const lm_matrix* a, int64_t rows, int64_t cols) {
-  need(a->rows == rows && a->cols == cols, std::string(what) + ": wrong shape");
+  need(a->rows == rows && a->cols == cols, what, "wrong shape");
 }
 
 // Memory of an argument: rows of `width` bytes, `pitch` bytes apart.
@@ -129,11 +131,15 @@ bool overlap(const Span& a, const Span& b) {
   }
   return true;
 }
+[[noreturn]] void overlapping(const Span& a, const Span& b) {
+  throw Bad{LM_ERR_INVALID_ARGUMENT, std::string(a.name) + " and " + b.name + " overlap"};
+}
 void apart(std::initializer_list<Span> outputs, std::initializer_list<Span> inputs) {
   for (auto o = outputs.begin(); o != outputs.end(); ++o) {
     for (auto p = outputs.begin(); p != o; ++p)
-      need(!overlap(*o, *p), std::string(o->name) + " and " + p->name + " overlap");
-    for (const Span& i : inputs) need(!overlap(*o, i), std::string(o->name) + " and " + i.name + " overlap");
+      if (overlap(*o, *p)) overlapping(*o, *p);
+    for (const Span& i : inputs)
+      if (overlap(*o, i)) overlapping(*o, i);
   }
 }
 bool same_place(const lm_matrix* a, const lm_matrix* b) { return a && b && a->data == b->data && a->ld == b->ld; }
@@ -187,10 +193,8 @@ void check_grid(int64_t a, int64_t b, int64_t c) {
   if (double(a) * double(b) * double(c) > double(kMaxGrid)) throw Bad{LM_ERR_UNSUPPORTED, "too many tiles for one launch"};
 }
 
-size_t partial_bytes(int64_t rows, int64_t count, int64_t n, int64_t k, int* splits) {
-  const int s = lm::weight_grad_splits(rows, count, n, k, lm::current_cus());
-  if (splits) *splits = s;
-  return s > 1 ? size_t(s) * size_t(count) * size_t(n) * size_t(k) * 4u : 0;
+size_t partial_bytes(int64_t rows, int64_t count, int64_t n, int64_t k) {
+  return size_t(lm::weight_grad_partials(rows, count, n, k, lm::current_cus())) * size_t(n) * size_t(k) * 4u;
 }
 
 }  // namespace
@@ -286,7 +290,7 @@ lm_status lionmuon_rmsnorm(const lm_matrix* x, const lm_matrix* residual, const 
       if (!others[i]) continue;
       check(names[i], others[i]);
       same_shape(names[i], others[i], x->rows, x->cols);
-      need(others[i]->dtype == x->dtype, std::string(names[i]) + " must have x's type");
+      need(others[i]->dtype == x->dtype, names[i], "wrong type");
     }
     if (kept) {
       check("checkpoint", kept);
@@ -344,7 +348,7 @@ lm_status lionmuon_rmsnorm_grad(const lm_matrix* dy, const lm_matrix* s,
       if (!others[i]) continue;
       check(names[i], others[i]);
       same_shape(names[i], others[i], dy->rows, dy->cols);
-      need(others[i]->dtype == dy->dtype, std::string(names[i]) + " must have dy's type");
+      need(others[i]->dtype == dy->dtype, names[i], "wrong type");
     }
     if (kept) {
       check("checkpoint", kept);
@@ -447,7 +451,7 @@ lm_status lionmuon_grouped_workspace_bytes(int64_t rows, int64_t count, int64_t 
     need(rows >= 0 && rows < (int64_t(1) << 30) && count >= 1 && count <= (int64_t(1) << 20) && n >= 1 && k >= 1 &&
              n < kMaxLd && k < kMaxLd,
          "bad size");
-    *out_bytes = partial_bytes(rows, count, n, k, nullptr);
+    *out_bytes = partial_bytes(rows, count, n, k);
     return hipSuccess;
   });
 }
@@ -477,8 +481,7 @@ lm_status lionmuon_grouped_weight_grad(const lm_matrix* dy, const lm_matrix* x,
         throw Bad{LM_ERR_UNSUPPORTED, "dy must be bf16 with a checkpoint (fp16 does not hold its values)"};
     }
     check_grid(dw->rows / 64 + 1, dw->cols / 64 + 1, dw->count);
-    int splits = 1;
-    const size_t wanted = partial_bytes(dy->rows, dw->count, dw->rows, dw->cols, &splits);
+    const size_t wanted = partial_bytes(dy->rows, dw->count, dw->rows, dw->cols);
     check_workspace(workspace, workspace_bytes, wanted);
     apart({span("dw", dw), span("workspace", workspace, 1, 0, int64_t(wanted))},
           {span("dy", dy), span("x", x), codes_span("codes", kept), scales_span("scales", kept),
@@ -500,7 +503,6 @@ lm_status lionmuon_grouped_weight_grad(const lm_matrix* dy, const lm_matrix* x,
     g.n = int32_t(dw->rows);
     g.k = int32_t(dw->cols);
     g.accumulate = accumulate;
-    g.splits = splits;
     g.partial = static_cast<float*>(workspace);
     g.cus = lm::current_cus();
     return lm::launch_grouped_weight_grad(elem(dy->dtype), g, stream);

@@ -83,26 +83,33 @@ __device__ __forceinline__ void copy16(u32x4 desc, uint32_t off, const void* dst
 // slots hold every tile and one look at the offsets finds a slot's expert: the last
 // one whose first slot is not behind it. Offsets are clamped to [0, rows], so wrong
 // ones cannot lead outside. Returns false for a slot without rows.
-struct RowTile {
-  int expert, row0, end;
-};
-template <int BM>
-__device__ __forceinline__ bool find_tile(const int32_t* offsets, int experts, int rows, int slot, RowTile* t) {
+__device__ __forceinline__ bool find_slot(const int32_t* offsets, int experts, int rows, int bm, int slot, int* expert, int* index) {
   const int lane = threadIdx.x & 63;
   int e = -1;
   for (int base = 0; base < experts; base += 64) {
     const int i = base + lane;
     const int off = min(max(offsets[min(i, experts - 1)], 0), rows);
-    const uint64_t m = __ballot(i < experts && off / BM + i <= slot);
+    const uint64_t m = __ballot(i < experts && off / bm + i <= slot);
     if (m == 0) break;
     e = base + 63 - __builtin_clzll(m);
   }
   e = __builtin_amdgcn_readfirstlane(e);
   if (e < 0) return false;
-  const int first = min(max(offsets[e], 0), rows), end = min(max(offsets[e + 1], 0), rows);
+  *expert = e;
+  *index = __builtin_amdgcn_readfirstlane(slot - (min(max(offsets[e], 0), rows) / bm + e));
+  return true;
+}
+
+struct RowTile {
+  int expert, row0, end;
+};
+template <int BM>
+__device__ __forceinline__ bool find_tile(const int32_t* offsets, int experts, int rows, int slot, RowTile* t) {
+  int e, i;
+  if (!find_slot(offsets, experts, rows, BM, slot, &e, &i)) return false;
   t->expert = e;
-  t->row0 = __builtin_amdgcn_readfirstlane(first + (slot - (first / BM + e)) * BM);
-  t->end = __builtin_amdgcn_readfirstlane(end);
+  t->row0 = __builtin_amdgcn_readfirstlane(min(max(offsets[e], 0), rows) + i * BM);
+  t->end = __builtin_amdgcn_readfirstlane(min(max(offsets[e + 1], 0), rows));
   return t->row0 < t->end;
 }
 
@@ -170,7 +177,8 @@ struct Source {
   bool wide;            // the matrix's rows hold at least eight elements
 };
 
-template <typename T, int MA, int MB, int BM, int BN, int WM, int WN, int NB, bool DMA>
+// DA, DB: the operand goes straight to LDS, else through registers.
+template <typename T, int MA, int MB, int BM, int BN, int WM, int WN, int NB, bool DA, bool DB>
 struct Tile {
   static constexpr int kWavesN = BN / WN, kWaves = (BM / WM) * kWavesN, kThreads = kWaves * 64;
   static constexpr int kMI = WM / 32, kNI = WN / 32;
@@ -264,22 +272,19 @@ struct Tile {
     }
   }
   template <int MODE, int W>
-  __device__ static __forceinline__ void put(const Source& s, int k0, const Regs<MODE, W>& r, char* dst, int tid) {
+  __device__ static __forceinline__ void put(const Source& s, int k0, const Regs<MODE, W>& r, int q, char* dst, int tid) {
     const bool cut = MODE == kRows ? s.depth - k0 < 64 && s.depth % 8 != 0 : s.cols < W && s.cols % 8 != 0;
-#pragma unroll
-    for (int q = 0; q < Regs<MODE, W>::kInst; ++q) {
-      int row, first;
-      const int n = present<MODE, W>(s, k0, q, tid, &row, &first);
-      u32x4 v = r.v[q];
-      if (cut) {      // (uniform) down by 8 - n elements
-        const int by = 8 - n;
-        if (by & 1) v = u32x4{(v[0] >> 16) | (v[1] << 16), (v[1] >> 16) | (v[2] << 16), (v[2] >> 16) | (v[3] << 16), v[3] >> 16};
-        if (by & 2) v = u32x4{v[1], v[2], v[3], 0u};
-        if (by & 4) v = u32x4{v[2], v[3], 0u, 0u};
-      }
-      if (n <= 0) v = u32x4{0u, 0u, 0u, 0u};
-      *reinterpret_cast<u32x4*>(dst + (q * kThreads + tid) * 16) = v;
+    int row, first;
+    const int n = present<MODE, W>(s, k0, q, tid, &row, &first);
+    u32x4 v = r.v[q];
+    if (cut) {      // (uniform) down by 8 - n elements
+      const int by = 8 - n;
+      if (by & 1) v = u32x4{(v[0] >> 16) | (v[1] << 16), (v[1] >> 16) | (v[2] << 16), (v[2] >> 16) | (v[3] << 16), v[3] >> 16};
+      if (by & 2) v = u32x4{v[1], v[2], v[3], 0u};
+      if (by & 4) v = u32x4{v[2], v[3], 0u, 0u};
     }
+    if (n <= 0) v = u32x4{0u, 0u, 0u, 0u};
+    *reinterpret_cast<u32x4*>(dst + (q * kThreads + tid) * 16) = v;
   }
 
   // A checkpoint's stage: 16 codes a load, widened to bf16 (exactly: the scale
@@ -356,7 +361,7 @@ struct Tile {
   // last step, says that every wave has read the stage (its buffer takes the stage NB
   // later) and that the next one has landed. Copies and fragment reads are
   // placed one behind each MFMA, so that the matrix unit never waits for a batch of
-  // them, and so are the codes' conversions.
+  // them, and so are the writes of what comes through registers.
   template <int FOLD>
   __device__ static __forceinline__ void product(const Source& a, const Source& b, const CodeSource& c, int depth, char* smem, f32x16 (&out)[kMI][kNI]) {
     const int tid = threadIdx.x, lane = tid & 63;
@@ -364,36 +369,47 @@ struct Tile {
     const int wm = (wave / kWavesN) * WM, wn = (wave % kWavesN) * WN;
     const int nk = (depth + 63) / 64;
     constexpr int kModeB = MB == kCodes ? int(kCols) : MB;
-    constexpr bool kDmaB = DMA && MB != kCodes;
-    constexpr int kCopiesA = DMA ? Copier<MA, BM>::kInst : 0, kCopiesB = kDmaB ? Copier<kModeB, BN>::kInst : 0;
+    static_assert(!(DB && MB == kCodes), "codes go through registers");
+    constexpr int kCopiesA = DA ? Copier<MA, BM>::kInst : 0, kCopiesB = DB ? Copier<kModeB, BN>::kInst : 0;
     constexpr int kCopies = kCopiesA + kCopiesB;
     constexpr int kPiecesB = MB == kCodes ? kPieces : 0;
-    constexpr int kCodeLoads = MB == kCodes ? 2 * CodeRegs::kInst : 0;
     Copier<MA, BM> ca(a, wave, lane);
     Copier<kModeB, BN> cb(b, wave, lane);
-    Regs<MA, DMA ? 0 : BM> ra;
-    Regs<kModeB, (DMA || MB == kCodes) ? 0 : BN> rb;
+    Regs<MA, DA ? 0 : BM> ra;
+    Regs<kModeB, (DB || MB == kCodes) ? 0 : BN> rb;
     CodeRegs rc;
     // stages that go through registers: loaded one stage ahead of the write to LDS
     auto load = [&](int kt) {
-      if constexpr (!DMA) fetch<MA, BM>(a, kt * 64, tid, ra);
-      if constexpr (!DMA && MB != kCodes) fetch<kModeB, BN>(b, kt * 64, tid, rb);
+      if constexpr (!DA) fetch<MA, BM>(a, kt * 64, tid, ra);
+      if constexpr (!DB && MB != kCodes) fetch<kModeB, BN>(b, kt * 64, tid, rb);
     };
     auto load_codes = [&](int kt) {
       if constexpr (MB == kCodes) fetch(c, kt * 64, tid, rc);
     };
-    auto write = [&](int kt, char* buf) {
-      if constexpr (!DMA) put<MA, BM>(a, kt * 64, ra, buf, tid);
-      if constexpr (!DMA && MB != kCodes) put<kModeB, BN>(b, kt * 64, rb, buf + BM * 128, tid);
+    constexpr int kWritesA = DA ? 0 : Regs<MA, BM>::kInst, kWritesB = (DB || MB == kCodes) ? 0 : Regs<kModeB, BN>::kInst;
+    constexpr int kWrites = kWritesA + kWritesB;
+    auto write = [&](int kt, int q, char* buf) {
+      if constexpr (!DA) {
+        if (q < kWritesA) {
+          put<MA, BM>(a, kt * 64, ra, q, buf, tid);
+          return;
+        }
+      }
+      if constexpr (!DB && MB != kCodes) put<kModeB, BN>(b, kt * 64, rb, q - kWritesA, buf + BM * 128, tid);
     };
     auto widen = [&](int piece, char* buf) { put(rc, piece, buf + BM * 128, tid); };
     auto start = [&](int kt) {
-      if constexpr (DMA) ca.start(kt * 64);
-      if constexpr (kDmaB) cb.start(kt * 64);
+      if constexpr (DA) ca.start(kt * 64);
+      if constexpr (DB) cb.start(kt * 64);
     };
     auto copy = [&](int q, char* buf) {
-      if (q < kCopiesA) ca.copy(q, buf, wave);
-      else cb.copy(q - kCopiesA, buf + BM * 128, wave);
+      if constexpr (DA) {
+        if (q < kCopiesA) {
+          ca.copy(q, buf, wave);
+          return;
+        }
+      }
+      if constexpr (DB) cb.copy(q - kCopiesA, buf + BM * 128, wave);
     };
     f32x16 acc[FOLD ? kMI : 1][FOLD ? kNI : 1];
     auto zero = [](auto& x) {
@@ -413,7 +429,8 @@ struct Tile {
       for (int q = 0; q < kCopies; ++q) copy(q, buf);
       if (kt < nk) {
         load(kt);
-        write(kt, buf);
+#pragma unroll
+        for (int q = 0; q < kWrites; ++q) write(kt, q, buf);
       }
       load_codes(kt);
 #pragma unroll
@@ -421,7 +438,7 @@ struct Tile {
     }
     if (NB < nk) load(NB);
     load_codes(NB);
-    if constexpr (DMA) wait_vmcnt<0>();
+    wait_vmcnt<0>();
     lds_barrier();
     s16x8 fa[2][kMI], fb[2][kNI];
     // fragment f of step kk (0..3) of the stage in `buf`: A's blocks, then B's
@@ -434,7 +451,7 @@ struct Tile {
     for (int f = 0; f < kFrags; ++f) read(0, smem, 0, f);
     // one step: its MFMAs, each followed by its share of the next step's reads (step
     // kk1 of the stage in `next`) and, in the last step, of what fills `fill`
-    auto step = [&](int kk, const char* next, int kk1, char* fill) {
+    auto step = [&](int kk, const char* next, int kk1, char* fill, int kt) {
       const int cur = kk & 1, nxt = cur ^ 1;
 #pragma unroll
       for (int m = 0; m < kMfmas; ++m) {
@@ -444,10 +461,21 @@ struct Tile {
 #pragma unroll
         for (int f = m * kFrags / kMfmas; f < (m + 1) * kFrags / kMfmas; ++f) read(nxt, next, kk1, f);
         if (kk == 3) {
+          // what comes through registers first: the wait for it would include
+          // copies that have just been started
+          constexpr int kHalf = kPiecesB + kWrites == 0 ? 0 : kCopies == 0 || kMfmas == 1 ? kMfmas : kMfmas / 2;
+          constexpr int kParts = kHalf > 0 ? kHalf : 1;
+          if (m < kHalf) {
 #pragma unroll
-          for (int q = m * kCopies / kMfmas; q < (m + 1) * kCopies / kMfmas; ++q) copy(q, fill);
+            for (int h = m * kPiecesB / kParts; h < (m + 1) * kPiecesB / kParts; ++h) widen(h, fill);
 #pragma unroll
-          for (int h = m * kPiecesB / kMfmas; h < (m + 1) * kPiecesB / kMfmas; ++h) widen(h, fill);
+            for (int q = m * kWrites / kParts; q < (m + 1) * kWrites / kParts; ++q) write(kt, q, fill);
+          }
+          if (m >= kHalf || kMfmas == 1) {
+            constexpr int kAt = kMfmas == 1 ? 0 : kHalf, kRest = kMfmas - kAt > 0 ? kMfmas - kAt : 1;
+#pragma unroll
+            for (int q = (m - kAt) * kCopies / kRest; q < (m - kAt + 1) * kCopies / kRest; ++q) copy(q, fill);
+          }
         }
         __builtin_amdgcn_sched_barrier(0);
       }
@@ -455,19 +483,19 @@ struct Tile {
     char* buf = smem;
     auto stage = [&](int kt) {
       char* next = buf == smem + (NB - 1) * kStageBytes ? smem : buf + kStageBytes;
-      step(0, buf, 1, buf);
-      step(1, buf, 2, buf);
-      step(2, buf, 3, buf);
-      // stage kt + 1 has landed: only copies of later ones, and the codes
-      // loaded after them, are still on their way
-      if constexpr (DMA) wait_vmcnt<(NB - 2) * (kCopies + kCodeLoads) + kCodeLoads>();
+      step(0, buf, 1, buf, 0);
+      step(1, buf, 2, buf, 0);
+      step(2, buf, 3, buf, 0);
+      // stage kt + 1 has landed: at least that many copies of later ones
+      // were started after its own
+      if constexpr (kCopies > 0) wait_vmcnt<(NB - 2) * kCopies>();
       lds_barrier();
       start(kt + NB);
-      if (kt + NB < nk) write(kt + NB, buf);
-      if (kt + NB + 1 < nk) load(kt + NB + 1);
       __builtin_amdgcn_sched_barrier(0);
-      step(3, next, 0, buf);
-      load_codes(kt + NB + 1);       // (their registers are free now)
+      step(3, next, 0, buf, kt + NB);
+      // (the registers are free now)
+      if (kt + NB + 1 < nk) load(kt + NB + 1);
+      load_codes(kt + NB + 1);
       __builtin_amdgcn_sched_barrier(0);
       buf = next;
     };
@@ -505,9 +533,9 @@ struct RowProduct {
   int vec_out;                        // rows of the output start 16-byte aligned
 };
 
-template <typename T, int MB, int BM, int BN, int WM, int WN, int NB, bool DMA>
-__global__ __launch_bounds__((BM / WM) * (BN / WN) * 64, BM * BN == 128 * 128 ? 2 : 1) void row_product_kernel(RowProduct g) {
-  using K = Tile<T, kRows, MB, BM, BN, WM, WN, NB, DMA>;
+template <typename T, int MB, int BM, int BN, int WM, int WN, int NB, bool DA, bool DB>
+__global__ __launch_bounds__((BM / WM) * (BN / WN) * 64, BM * BN <= 128 * 128 ? 2 : 1) void row_product_kernel(RowProduct g) {
+  using K = Tile<T, kRows, MB, BM, BN, WM, WN, NB, DA, DB>;
   constexpr int kStage = 32 * (WN + 8);         // elements of a wave's output staging
   static_assert(K::kWaves * kStage * 2 <= K::kLds, "staging fits");
   __shared__ __align__(16) char smem[K::kLds];
@@ -581,31 +609,45 @@ struct WeightProduct {
   const void* x;
   CkptView kept;
   const int32_t* offsets;
-  float* out;                         // dW, or the partials of the splits
+  float* out;                         // dW
+  float* partial;                     // tiles of experts in several parts: slots x n x k
   int64_t lddy, ldx, ldo, o_stride;   // elements; o_stride: of an expert
-  int64_t split_stride;               // partials: of a split
   int rows, experts, n, k;
-  int tiles_m, tiles_n, splits, chunk;
+  int tiles_m, tiles_n, chunk;
+  int part;                           // rows of a part of an expert; > rows: whole experts
+  int units;
   int accumulate;
 };
 
-template <typename T, int MB, int BM, int BN, int WM, int WN, int NB, bool DMA>
-__global__ __launch_bounds__((BM / WM) * (BN / WN) * 64, BM * BN == 128 * 128 ? 2 : 1) void weight_product_kernel(WeightProduct g) {
-  using K = Tile<T, kCols, MB, BM, BN, WM, WN, NB, DMA>;
+// Experts of more than `part` rows go to several workgroups, `part` rows each, whose
+// sums meet in weight_reduce_kernel. Their partial sums need
+// ceil(len / part) slots each; counting an expert's from floor(2 offset / part) keeps
+// them apart (for len > part, ceil(len / part) <= floor(2 end / part) - floor(2 offset / part))
+// and needs 2 rows / part + 1 in all.
+__device__ __forceinline__ int partial_slot(int first, int part) { return int(2 * int64_t(first) / part); }
+
+template <typename T, int MB, int BM, int BN, int WM, int WN, int NB, bool DA, bool DB>
+__global__ __launch_bounds__((BM / WM) * (BN / WN) * 64, BM * BN <= 128 * 128 ? 2 : 1) void weight_product_kernel(WeightProduct g) {
+  using K = Tile<T, kCols, MB, BM, BN, WM, WN, NB, DA, DB>;
   __shared__ __align__(16) char smem[K::kLds];
   const int per = g.tiles_m * g.tiles_n;
   const int id = by_xcd(blockIdx.x, g.chunk), unit = id / per;
-  if (unit >= g.experts * g.splits) return;
+  if (unit >= g.units) return;
   int tm, tn;
   banded(id - unit * per, g.tiles_m, g.tiles_n, &tm, &tn);
-  const int nth = unit / g.splits, s = unit - nth * g.splits;
-  const int e = nth_longest(g.offsets, g.experts, g.rows, nth);
+  int e, i = 0;
+  if (g.part > g.rows) {
+    e = nth_longest(g.offsets, g.experts, g.rows, unit);
+  } else {
+    // as in find_tile; every expert has a first part, if an empty one
+    if (!find_slot(g.offsets, g.experts, g.rows, g.part, unit, &e, &i)) return;
+  }
   const int first = min(max(g.offsets[e], 0), g.rows), end = min(max(g.offsets[e + 1], 0), g.rows);
-  // this split's rows: whole stages, the same number for every split
   const int len = max(end - first, 0);
-  const int each = ((len + 63) / 64 + g.splits - 1) / g.splits * 64;
-  const int row0 = __builtin_amdgcn_readfirstlane(first + min(s * each, len));
-  const int depth = __builtin_amdgcn_readfirstlane(min(each, first + len - row0));
+  if (i > 0 && int64_t(i) * g.part >= len) return;
+  const int row0 = __builtin_amdgcn_readfirstlane(first + i * g.part);
+  const int depth = __builtin_amdgcn_readfirstlane(min(g.part, len - i * g.part));
+  const bool whole = len <= g.part;
   const int m0 = tm * BM, n0 = tn * BN;
   Source a, b;
   typename K::CodeSource c;
@@ -635,7 +677,9 @@ __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64, BM * BN == 128 * 128 ? 
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wm = (wave / K::kWavesN) * WM, wn = (wave % K::kWavesN) * WN;
-  float* out = g.out + s * g.split_stride + e * g.o_stride;
+  float* out = whole ? g.out + e * g.o_stride : g.partial + int64_t(partial_slot(first, g.part) + i) * g.n * g.k;
+  const int64_t ldo = whole ? g.ldo : g.k;
+  const bool add = whole && g.accumulate;
   // 32 lanes write 128 bytes of a row
 #pragma unroll
   for (int i = 0; i < K::kMI; ++i)
@@ -646,31 +690,52 @@ __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64, BM * BN == 128 * 128 ? 
       for (int r = 0; r < 16; ++r) {
         const int row = m0 + wm + 32 * i + 8 * (r >> 2) + 4 * (lane >> 5) + (r & 3);
         if (row < g.n && col < g.k) {
-          float* p = out + int64_t(row) * g.ldo + col;
-          *p = g.accumulate ? *p + acc[i][j][r] : acc[i][j][r];
+          float* p = out + int64_t(row) * ldo + col;
+          *p = add ? *p + acc[i][j][r] : acc[i][j][r];
         }
       }
     }
 }
 
-// dW = (dW +) the sum of the splits' partials, in their order: four columns a
-// thread, `blocks` workgroups a row of dW.
-__global__ __launch_bounds__(256) void weight_reduce_kernel(const float* partial, int splits, int64_t per_split, float* out, int64_t ldo, int64_t o_stride, int n, int k, int blocks, int accumulate) {
-  const int line = blockIdx.x / blocks, col = ((blockIdx.x - line * blocks) * 256 + threadIdx.x) * 4;
-  if (col >= k) return;
-  const int e = line / n, row = line - e * n;
-  const float* p = partial + int64_t(line) * k + col;
-  float* o = out + e * o_stride + row * ldo + col;
-  float v[4] = {0.f, 0.f, 0.f, 0.f};
-  const int m = min(4, k - col);
-  for (int s = 0; s < splits; ++s) {
-#pragma unroll
-    for (int j = 0; j < 4; ++j)
-      if (j < m) v[j] += p[int64_t(s) * per_split + j];
+// dW_e = (dW_e +) the sum of the parts of an expert that has several, in their
+// order: four columns a thread, `blocks` workgroups a row of dW. Workgroups of
+// the nth such expert, of at most rows / part.
+__global__ __launch_bounds__(256) void weight_reduce_kernel(WeightProduct g, int blocks) {
+  const int line = blockIdx.x / blocks, nth = line / g.n, row = line - nth * g.n;
+  const int lane = threadIdx.x & 63;
+  int e = -1, seen = 0;
+  for (int base = 0; base < g.experts; base += 64) {
+    const int i = min(base + lane, g.experts - 1);
+    const int len = min(max(g.offsets[i + 1], 0), g.rows) - min(max(g.offsets[i], 0), g.rows);
+    uint64_t m = __ballot(base + lane < g.experts && len > g.part);
+    const int here = __builtin_popcountll(m);
+    if (seen + here > nth) {
+      for (int j = seen; j < nth; ++j) m &= m - 1;
+      e = base + __builtin_ctzll(m);
+      break;
+    }
+    seen += here;
   }
+  if (e < 0) return;
+  const int first = min(max(g.offsets[e], 0), g.rows), len = min(max(g.offsets[e + 1], 0), g.rows) - first;
+  const int parts = (len + g.part - 1) / g.part;
+  const int col = ((blockIdx.x - line * blocks) * 256 + threadIdx.x) * 4, m = min(4, g.k - col);
+  if (m <= 0) return;
+  const int64_t one = int64_t(g.n) * g.k;
+  const float* p = g.partial + partial_slot(first, g.part) * one + int64_t(row) * g.k + col;
+  float* o = g.out + e * g.o_stride + row * g.ldo + col;
+  float v[4] = {0.f, 0.f, 0.f, 0.f};
+  for (int s = 0; s < parts; ++s) {
+    if (m == 4) {
+      float t[4];
+      __builtin_memcpy(t, p + s * one, 16);
 #pragma unroll
-  for (int j = 0; j < 4; ++j)
-    if (j < m) o[j] = accumulate ? o[j] + v[j] : v[j];
+      for (int j = 0; j < 4; ++j) v[j] += t[j];
+    } else {
+      for (int j = 0; j < m; ++j) v[j] += p[s * one + j];
+    }
+  }
+  for (int j = 0; j < m; ++j) o[j] = g.accumulate ? o[j] + v[j] : v[j];
 }
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
@@ -678,8 +743,76 @@ bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 
 // Grid of `tiles` tiles in runs of `chunk`, a multiple of eight of them.
 unsigned grid_of(int64_t tiles, int64_t chunk) { return unsigned((tiles + 8 * chunk - 1) / (8 * chunk) * 8 * chunk); }
 
+// ---------------------------------------------------------------------------
+// Choice of tiles
+// ---------------------------------------------------------------------------
+// Microseconds of a stage of 64 contraction values where every CU has its
+// `at_once` tiles, and of a tile besides (start and output).
+struct TileCost {
+  int bm, bn, at_once;
+  double stage, rest;
+};
+constexpr TileCost kRowTiles[3] = {{256, 256, 1, 1.05, 6.0}, {128, 128, 2, 0.62, 4.0}, {64, 64, 2, 0.30, 3.0}};
+constexpr TileCost kWeightTiles[3] = {{256, 128, 1, 0.62, 6.0}, {128, 128, 2, 0.75, 5.0}, {64, 64, 2, 0.35, 3.0}};
+
+int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+// Tile of a row product: the least time by rounds of tiles over the CUs. An
+// expert's last tile is half empty on average.
+int row_tile(int64_t rows, int64_t experts, int64_t width, int64_t depth, int cus) {
+  int best = 0;
+  double least = 0.0;
+  for (int i = 0; i < 3; ++i) {
+    const TileCost& c = kRowTiles[i];
+    const int64_t tiles = (rows / c.bm + std::min<int64_t>(experts, rows) / 2 + 1) * ceil_div(width, c.bn);
+    const double t = double(ceil_div(tiles, int64_t(cus) * c.at_once)) * (c.stage * double(ceil_div(depth, 64)) + c.rest);
+    if (i == 0 || t < least) {
+      best = i;
+      least = t;
+    }
+  }
+  return best;
+}
+
+// Tile of a weight gradient and the rows of a part (WeightProduct). Whole
+// experts cost the longest one's rows, taken as three times the mean; parts as long as an even
+// share of the rows, and 12 bytes of traffic for each partial value at 4 TB/s.
+struct WeightPlan {
+  int tile;
+  int64_t part;
+};
+WeightPlan weight_plan(int64_t rows, int64_t experts, int64_t n, int64_t k, int cus) {
+  WeightPlan best{0, rows + 1};
+  double least = -1.0;
+  for (int i = 0; i < 3; ++i) {
+    const TileCost& c = kWeightTiles[i];
+    const int64_t per = ceil_div(n, c.bm) * ceil_div(k, c.bn);
+    const double share = double(rows) * double(per) / double(int64_t(cus) * c.at_once);   // rows of a tile's place
+    const double longest = experts == 1 ? double(rows) : std::min(double(rows), 3.0 * double(rows) / double(experts));
+    const double rounds = std::max(1.0, double(experts * per) / double(int64_t(cus) * c.at_once));
+    const double whole = std::max(share, longest) / 64.0 * c.stage + rounds * c.rest;
+    if (least < 0.0 || whole < least) {
+      least = whole;
+      best = WeightPlan{i, rows + 1};
+    }
+    const int64_t part = std::max<int64_t>(256, ceil_div(int64_t(share) + 1, 64) * 64);
+    if (double(part) < longest / 1.25) {
+      const double parts = double(rows) / double(part) + (experts == 1 ? 1.0 : 0.0);
+      const double split = 1.3 * double(part) / 64.0 * c.stage + rounds * c.rest + parts * double(n) * double(k) * 12.0 / 4e6 + 6.0;
+      if (split < least) {
+        least = split;
+        best = WeightPlan{i, part};
+      }
+    }
+  }
+  return best;
+}
+
+// Slots of partial sums that parts of that many rows can need.
+int64_t partial_slots(int64_t rows, int64_t part) { return part > rows ? 0 : 2 * rows / part + 1; }
+
 template <typename T, int MB, int BM, int BN, int WM, int WN, int NB>
-void run_rows(RowProduct g, bool dma, hipStream_t stream) {
+void run_rows(RowProduct g, bool da, bool db, hipStream_t stream) {
   g.slots = g.rows / BM + g.experts;
   g.tiles_n = (g.width + BN - 1) / BN;
   // one run an XCD: tiles cost the same
@@ -687,8 +820,21 @@ void run_rows(RowProduct g, bool dma, hipStream_t stream) {
   g.chunk = int((tiles + 7) / 8);
   const dim3 grid(grid_of(tiles, g.chunk));
   constexpr int kThreads = (BM / WM) * (BN / WN) * 64;
-  if (dma) row_product_kernel<T, MB, BM, BN, WM, WN, NB, true><<<grid, kThreads, 0, stream>>>(g);
-  else row_product_kernel<T, MB, BM, BN, WM, WN, NB, false><<<grid, kThreads, 0, stream>>>(g);
+  if (da && db) {
+    row_product_kernel<T, MB, BM, BN, WM, WN, NB, true, true><<<grid, kThreads, 0, stream>>>(g);
+    return;
+  }
+  if constexpr (MB == kCols) {       // (rows of Y = X W^T's operands are alike)
+    if (db) {
+      row_product_kernel<T, MB, BM, BN, WM, WN, NB, false, true><<<grid, kThreads, 0, stream>>>(g);
+      return;
+    }
+    if (da) {
+      row_product_kernel<T, MB, BM, BN, WM, WN, NB, true, false><<<grid, kThreads, 0, stream>>>(g);
+      return;
+    }
+  }
+  row_product_kernel<T, MB, BM, BN, WM, WN, NB, false, false><<<grid, kThreads, 0, stream>>>(g);
 }
 
 template <typename T, int MB>
@@ -709,46 +855,65 @@ void row_product(const GroupArgs& x, int width, int depth, hipStream_t stream) {
   g.vec_out = aligned16(x.c) && x.ldc % 8 == 0;
   // copies straight to LDS need rows on 16 bytes, and a contraction in whole
   // chunks where an operand runs along it
-  const bool dma = aligned16(x.a) && aligned16(x.b) && x.lda % 8 == 0 && x.ldb % 8 == 0 && x.b_stride % 8 == 0 && depth % 8 == 0;
-  if (x.rows / x.experts >= 192) run_rows<T, MB, 256, 256, 128, 128, 2>(g, dma, stream);
-  else run_rows<T, MB, 128, 128, 64, 64, 2>(g, dma, stream);
+  const bool da = aligned16(x.a) && x.lda % 8 == 0 && depth % 8 == 0;
+  const bool db = aligned16(x.b) && x.ldb % 8 == 0 && x.b_stride % 8 == 0 && (MB == kCols || depth % 8 == 0);
+  switch (row_tile(x.rows, x.experts, width, depth, x.cus)) {
+    case 0: run_rows<T, MB, 256, 256, 128, 128, 2>(g, da, db, stream); break;
+    case 1: run_rows<T, MB, 128, 128, 64, 64, 2>(g, da, db, stream); break;
+    default: run_rows<T, MB, 64, 64, 32, 32, 4>(g, da, db, stream); break;
+  }
+}
+
+template <typename T, int MB, int BM, int BN, int WM, int WN, int NB>
+void run_weight(WeightProduct g, bool da, bool db, hipStream_t stream) {
+  g.tiles_m = (g.n + BM - 1) / BM;
+  g.tiles_n = (g.k + BN - 1) / BN;
+  // an expert's tiles over all XCDs: those of one expert cost the same
+  const int64_t per = int64_t(g.tiles_m) * g.tiles_n;
+  g.chunk = int((per + 7) / 8);
+  const dim3 grid(grid_of(per * g.units, g.chunk));
+  constexpr int kThreads = (BM / WM) * (BN / WN) * 64;
+  if constexpr (MB == kCodes) {
+    if (da) weight_product_kernel<T, MB, BM, BN, WM, WN, NB, true, false><<<grid, kThreads, 0, stream>>>(g);
+    else weight_product_kernel<T, MB, BM, BN, WM, WN, NB, false, false><<<grid, kThreads, 0, stream>>>(g);
+  } else {
+    if (da && db) weight_product_kernel<T, MB, BM, BN, WM, WN, NB, true, true><<<grid, kThreads, 0, stream>>>(g);
+    else if (db) weight_product_kernel<T, MB, BM, BN, WM, WN, NB, false, true><<<grid, kThreads, 0, stream>>>(g);
+    else if (da) weight_product_kernel<T, MB, BM, BN, WM, WN, NB, true, false><<<grid, kThreads, 0, stream>>>(g);
+    else weight_product_kernel<T, MB, BM, BN, WM, WN, NB, false, false><<<grid, kThreads, 0, stream>>>(g);
+  }
 }
 
 template <typename T, int MB>
 void weight_product(const GroupArgs& x, hipStream_t stream) {
-  constexpr int BM = 256, BN = 128, WM = 128, WN = 64, NB = 3;
+  const WeightPlan plan = weight_plan(x.rows, x.experts, x.n, x.k, x.cus);
   WeightProduct g;
   g.dy = x.a;
   g.x = x.b;
   g.kept = x.kept;
   g.offsets = x.offsets;
+  g.out = static_cast<float*>(x.c);
+  g.partial = x.partial;
   g.lddy = x.lda;
   g.ldx = x.ldb;
+  g.ldo = x.ldc;
+  g.o_stride = x.c_stride;
   g.rows = int(x.rows);
   g.experts = x.experts;
   g.n = x.n;
   g.k = x.k;
-  g.tiles_m = (x.n + BM - 1) / BM;
-  g.tiles_n = (x.k + BN - 1) / BN;
-  g.splits = x.splits;
-  const int64_t one = int64_t(x.n) * x.k;
-  const bool split = x.splits > 1;
-  g.out = split ? x.partial : static_cast<float*>(x.c);
-  g.ldo = split ? x.k : x.ldc;
-  g.o_stride = split ? one : x.c_stride;
-  g.split_stride = split ? one * x.experts : 0;
-  g.accumulate = split ? 0 : x.accumulate;
-  // an expert's tiles over all XCDs: those of one expert cost the same
-  const int64_t per = int64_t(g.tiles_m) * g.tiles_n;
-  g.chunk = int((per + 7) / 8);
-  const dim3 grid(grid_of(per * x.experts * x.splits, g.chunk));
-  const bool dma = aligned16(x.a) && x.lda % 8 == 0 && (MB == kCodes || (aligned16(x.b) && x.ldb % 8 == 0));
-  if (dma) weight_product_kernel<T, MB, BM, BN, WM, WN, NB, true><<<grid, 256, 0, stream>>>(g);
-  else weight_product_kernel<T, MB, BM, BN, WM, WN, NB, false><<<grid, 256, 0, stream>>>(g);
-  if (split) {
-    const int blocks = (x.k + 1023) / 1024;
-    weight_reduce_kernel<<<dim3(unsigned(int64_t(blocks) * x.n * x.experts)), 256, 0, stream>>>(
-        x.partial, x.splits, one * x.experts, static_cast<float*>(x.c), x.ldc, x.c_stride, x.n, x.k, blocks, x.accumulate);
+  g.accumulate = x.accumulate;
+  g.part = int(plan.part);
+  g.units = int(x.rows / plan.part) + x.experts;
+  const bool da = aligned16(x.a) && x.lda % 8 == 0, db = MB != kCodes && aligned16(x.b) && x.ldb % 8 == 0;
+  switch (plan.tile) {
+    case 0: run_weight<T, MB, 256, 128, 128, 64, 3>(g, da, db, stream); break;
+    case 1: run_weight<T, MB, 128, 128, 64, 64, 2>(g, da, db, stream); break;
+    default: run_weight<T, MB, 64, 64, 32, 32, 4>(g, da, db, stream); break;
+  }
+  if (plan.part <= x.rows) {
+    const int64_t blocks = ceil_div(x.k, 1024);
+    weight_reduce_kernel<<<dim3(unsigned(blocks * x.n * (x.rows / plan.part))), 256, 0, stream>>>(g, int(blocks));
   }
 }
 
@@ -773,14 +938,8 @@ hipError_t launch_grouped_weight_grad(Elem t, const GroupArgs& g, hipStream_t st
   return hipGetLastError();
 }
 
-// Row ranges of an expert: as many as it takes to give every CU two tiles, of at
-// least 1024 rows each on average (a partial costs 8 bytes of traffic an
-// element, 1024 rows of contraction about 40 times that in matrix time).
-int32_t weight_grad_splits(int64_t rows, int64_t experts, int64_t n, int64_t k, int cus) {
-  const int64_t tiles = ((n + 255) / 256) * ((k + 127) / 128) * experts;
-  const int64_t want = (2 * int64_t(cus) + tiles - 1) / tiles, most = rows / experts / 1024;
-  const int64_t s = want < most ? want : most;
-  return int32_t(s < 1 ? 1 : s);
+int64_t weight_grad_partials(int64_t rows, int64_t experts, int64_t n, int64_t k, int cus) {
+  return partial_slots(rows, weight_plan(rows, experts, n, k, cus).part);
 }
 
 }  // namespace lm

@@ -92,7 +92,7 @@ class Checkpoint:
     byte e + 127 for each 128 columns of a row); a code stands for its
     e4m3 value times 2^e."""
 
-    __slots__ = ("codes", "scales")
+    __slots__ = ("shape", "device", "_desc", "_buffer", "_codes", "_scales")
 
     def __init__(self, codes, scales):
         for t, name in ((codes, "codes"), (scales, "scales")):
@@ -100,142 +100,168 @@ class Checkpoint:
                 raise TypeError(f"{name} must be a torch.Tensor")
             if t.dtype != torch.uint8 or t.dim() != 2:
                 _invalid(f"{name} must be a 2-D uint8 tensor")
-        if scales.shape != (codes.shape[0], -(-codes.shape[1] // CHECKPOINT_BLOCK)):
+        rows, cols = codes.shape
+        blocks = -(-cols // CHECKPOINT_BLOCK)
+        if scales.shape != (rows, blocks):
             _invalid("scales must hold one byte for each 128 columns of a row")
         if codes.device != scales.device:
             _invalid("codes and scales must be on one device")
-        self.codes = codes
-        self.scales = scales
+        ld, step = codes.stride()
+        ld_scales, step_scales = scales.stride()
+        if (cols > 1 and step != 1) or (blocks > 1 and step_scales != 1):
+            _invalid("the rows of codes and scales must be contiguous")
+        self.shape = codes.shape
+        self.device = codes.device
+        self._buffer = None
+        self._codes = codes
+        self._scales = scales
+        self._desc = lm_checkpoint(codes.data_ptr(), scales.data_ptr(), rows, cols,
+                                   ld if rows > 1 else -(-cols // 16) * 16,
+                                   ld_scales if rows > 1 else blocks)
 
     @classmethod
-    def empty(cls, rows, cols, device=None):
-        """An uninitialised checkpoint (filled by the operators that write one)."""
-        codes = torch.empty(rows, -(-cols // 16) * 16, dtype=torch.uint8, device=device or "cuda")
-        scales = torch.empty(rows, -(-cols // CHECKPOINT_BLOCK), dtype=torch.uint8,
-                             device=codes.device)
-        return cls(codes[:, :cols], scales)
+    def empty(cls, rows, cols, device="cuda"):
+        """An uninitialised checkpoint (filled by the operators that write one):
+        its codes and scales lie in one allocation."""
+        ld, blocks = -(-cols // 16) * 16, -(-cols // CHECKPOINT_BLOCK)
+        self = cls.__new__(cls)
+        self._buffer = buffer = torch.empty(rows * (ld + blocks), dtype=torch.uint8, device=device)
+        self.shape = torch.Size((rows, cols))
+        self.device = buffer.device
+        self._codes = self._scales = None
+        base = buffer.data_ptr()
+        self._desc = lm_checkpoint(base, base + rows * ld if base else 0, rows, cols, ld, blocks)
+        return self
 
     @property
-    def shape(self):
-        return self.codes.shape
+    def codes(self):
+        if self._codes is None:
+            rows, ld = self._desc.rows, self._desc.ld_codes
+            self._codes = self._buffer[:rows * ld].view(rows, ld)[:, :self._desc.cols]
+        return self._codes
 
     @property
-    def device(self):
-        return self.codes.device
+    def scales(self):
+        if self._scales is None:
+            rows, d = self._desc.rows, self._desc
+            self._scales = self._buffer[rows * d.ld_codes:].view(rows, d.ld_scales)
+        return self._scales
 
 
 # -- marshalling -------------------------------------------------------------
-def _matrix(t, name, device=None):
+def _device_of(t, name):
     if not isinstance(t, torch.Tensor):
         raise TypeError(f"{name} must be a torch.Tensor")
-    if not t.is_cuda:
+    device = t.device
+    if device.type != "cuda":
         _invalid(f"{name} must be a GPU tensor")
-    if device is not None and t.device != device:
+    return device
+
+
+def _check_place(t, name, device):
+    if _device_of(t, name) != device:
         _invalid(f"{name} is on {t.device}, the other tensors are on {device}")
-    if t.dim() != 2:
-        _invalid(f"{name} must be 2-D")
+
+
+def _matrix(t, name, device):
+    if not isinstance(t, torch.Tensor) or t.device != device:
+        _check_place(t, name, device)
     code = _DTYPES.get(t.dtype)
     if code is None:
         _invalid(f"{name} must be float32, bfloat16 or float16")
+    if t.dim() != 2:
+        _invalid(f"{name} must be 2-D")
     rows, cols = t.shape
     ld, step = t.stride()
-    if cols > 1 and step != 1:
+    if step != 1 and cols > 1:
         _invalid(f"the rows of {name} must be contiguous")
     return lm_matrix(t.data_ptr(), rows, cols, ld if rows > 1 else cols, code, 0)
 
 
+def _new(rows, cols, like, code):
+    """A new contiguous matrix of like's type and its descriptor."""
+    t = torch.empty((rows, cols), dtype=like.dtype, device=like.device)
+    return t, lm_matrix(t.data_ptr(), rows, cols, cols, code, 0)
+
+
 def _stack(t, name, device):
-    if not isinstance(t, torch.Tensor):
-        raise TypeError(f"{name} must be a torch.Tensor")
-    if not t.is_cuda or t.device != device:
-        _invalid(f"{name} must be on {device}")
-    if t.dim() != 3:
-        _invalid(f"{name} must be 3-D (experts, n, k)")
+    if not isinstance(t, torch.Tensor) or t.device != device:
+        _check_place(t, name, device)
     code = _DTYPES.get(t.dtype)
     if code is None:
         _invalid(f"{name} must be float32, bfloat16 or float16")
+    if t.dim() != 3:
+        _invalid(f"{name} must be 3-D (experts, n, k)")
     count, rows, cols = t.shape
     stride, ld, step = t.stride()
-    if cols > 1 and step != 1:
+    if step != 1 and cols > 1:
         _invalid(f"the rows of {name} must be contiguous")
-    ld = ld if rows > 1 else cols
-    return lm_stack(t.data_ptr(), count, rows, cols, ld,
-                    stride if count > 1 else rows * ld, code, 0)
+    if rows <= 1:
+        ld = cols
+    return lm_stack(t.data_ptr(), count, rows, cols, ld, stride if count > 1 else rows * ld,
+                    code, 0)
 
 
 def _codes(c, name, device):
     if not isinstance(c, Checkpoint):
         raise TypeError(f"{name} must be a Checkpoint")
-    if not c.codes.is_cuda or c.codes.device != device:
-        _invalid(f"{name} must be on {device}")
-    rows, cols = c.codes.shape
-    ld, step = c.codes.stride()
-    ld_scales, step_scales = c.scales.stride()
-    blocks = c.scales.shape[1]
-    if (cols > 1 and step != 1) or (blocks > 1 and step_scales != 1):
-        _invalid(f"the rows of {name} must be contiguous")
-    return lm_checkpoint(c.codes.data_ptr(), c.scales.data_ptr(), rows, cols,
-                         ld if rows > 1 else -(-cols // 16) * 16,
-                         ld_scales if rows > 1 else blocks)
+    if c.device != device:
+        _invalid(f"{name} is on {c.device}, the other tensors are on {device}")
+    return c._desc
+
+
+def _wanted(checkpoint, rows, cols, device):
+    """The Checkpoint to write: None, a new one, or the one passed in."""
+    if checkpoint is False or checkpoint is None:
+        return None
+    if isinstance(checkpoint, Checkpoint):
+        _codes(checkpoint, "checkpoint", device)
+        return checkpoint
+    return Checkpoint.empty(rows, cols, device)
 
 
 def _vector(t, n, name, device):
-    if not isinstance(t, torch.Tensor):
-        raise TypeError(f"{name} must be a torch.Tensor")
-    if not t.is_cuda or t.device != device:
-        _invalid(f"{name} must be on {device}")
-    if t.dtype != torch.float32 or t.shape != (n,) or not t.is_contiguous():
+    if not isinstance(t, torch.Tensor) or t.device != device:
+        _check_place(t, name, device)
+    if t.dtype != torch.float32 or t.dim() != 1 or t.shape[0] != n or not t.is_contiguous():
         _invalid(f"{name} must be a contiguous float32 tensor of {n} values")
     return t.data_ptr()
 
 
 def _offsets(t, experts, device):
-    if not isinstance(t, torch.Tensor):
-        raise TypeError("offsets must be a torch.Tensor")
-    if not t.is_cuda or t.device != device:
-        _invalid(f"offsets must be on {device}")
-    if t.dtype != torch.int32 or t.shape != (experts + 1,) or not t.is_contiguous():
+    if not isinstance(t, torch.Tensor) or t.device != device:
+        _check_place(t, "offsets", device)
+    if t.dtype != torch.int32 or t.dim() != 1 or t.shape[0] != experts + 1 or \
+            not t.is_contiguous():
         _invalid(f"offsets must be a contiguous int32 tensor of {experts + 1} values")
     return t.data_ptr()
 
 
-def _ref(x):
-    return None if x is None else ctypes.byref(x)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or \
+    (lambda index: torch.cuda.current_stream(index).cuda_stream)
+
+
+def _here(device, stream):
+    """Handle of the current stream if that is where the call goes, else None."""
+    if stream is None and torch.cuda.current_device() == device.index:
+        return _raw_stream(device.index)
+    return None
 
 
 @contextlib.contextmanager
 def _switched(device, stream):
+    """Makes the tensors' device and the call's stream current, so that what torch
+    allocates for the call belongs to that stream."""
     with torch.cuda.device(device):
         if stream is None:
-            yield torch.cuda.current_stream().cuda_stream
+            yield
             return
         if not hasattr(stream, "cuda_stream"):
             stream = torch.cuda.ExternalStream(int(stream), device=device)
         elif stream.device != device:
             _invalid(f"stream is on {stream.device}, the tensors are on {device}")
-        # what torch allocates for the call belongs to the call's stream
         with torch.cuda.stream(stream):
-            yield stream.cuda_stream
-
-
-@contextlib.contextmanager
-def _unswitched(handle):
-    yield handle
-
-
-def _stream(device, stream):
-    """Context in which a call on `device` and `stream` allocates and launches."""
-    if stream is None and torch.cuda.current_device() == device.index:
-        return _unswitched(torch.cuda.current_stream().cuda_stream)
-    return _switched(device, stream)
-
-
-def _device_of(t, name):
-    if not isinstance(t, torch.Tensor):
-        raise TypeError(f"{name} must be a torch.Tensor")
-    if not t.is_cuda:
-        _invalid(f"{name} must be a GPU tensor")
-    return t.device
+            yield
 
 
 def _done(status, what):
@@ -247,12 +273,14 @@ def _done(status, what):
 def lionmuon_checkpoint(x, out: Checkpoint | None = None, stream=None) -> Checkpoint:
     """8-bit checkpoint of a 2-D float32, bfloat16 or float16 tensor."""
     device = _device_of(x, "x")
-    mx = _matrix(x, "x")
-    with _stream(device, stream) as handle:
-        if out is None:
-            out = Checkpoint.empty(mx.rows, mx.cols, device)
-        _done(_lib().lionmuon_checkpoint(mx, _codes(out, "out", device), handle),
-              "lionmuon_checkpoint")
+    handle = _here(device, stream)
+    if handle is None:
+        with _switched(device, stream):
+            return lionmuon_checkpoint(x, out)
+    m = _matrix(x, "x", device)
+    if out is None:
+        out = Checkpoint.empty(m.rows, m.cols, device)
+    _done(_lib().lionmuon_checkpoint(m, _codes(out, "out", device), handle), "lionmuon_checkpoint")
     return out
 
 
@@ -261,21 +289,26 @@ def lionmuon_checkpoint_restore(checkpoint: Checkpoint, dtype=torch.bfloat16, ou
     """The values of a checkpoint, in ``dtype`` (exact in float32 and bfloat16)."""
     if not isinstance(checkpoint, Checkpoint):
         raise TypeError("checkpoint must be a Checkpoint")
-    device = _device_of(checkpoint.codes, "checkpoint")
-    with _stream(device, stream) as handle:
-        if out is None:
-            out = torch.empty(checkpoint.shape, dtype=dtype, device=device)
-        _done(_lib().lionmuon_checkpoint_restore(_codes(checkpoint, "checkpoint", device),
-                                                 _matrix(out, "out", device), handle),
-              "lionmuon_checkpoint_restore")
+    device = checkpoint.device
+    if device.type != "cuda":
+        _invalid("checkpoint must be on a GPU")
+    handle = _here(device, stream)
+    if handle is None:
+        with _switched(device, stream):
+            return lionmuon_checkpoint_restore(checkpoint, dtype, out)
+    if out is None:
+        out = torch.empty(checkpoint.shape, dtype=dtype, device=device)
+    _done(_lib().lionmuon_checkpoint_restore(checkpoint._desc, _matrix(out, "out", device), handle),
+          "lionmuon_checkpoint_restore")
     return out
 
 
 # -- activation functions ----------------------------------------------------
 def _kind(kind):
-    if kind not in ACTIVATIONS:
+    code = ACTIVATIONS.get(kind)
+    if code is None:
         raise ValueError(f"unknown activation {kind!r}: one of {sorted(ACTIVATIONS)}")
-    return ACTIVATIONS[kind]
+    return code
 
 
 def lionmuon_activation(a, kind, out=None, checkpoint=False, stream=None):
@@ -284,23 +317,22 @@ def lionmuon_activation(a, kind, out=None, checkpoint=False, stream=None):
     ``checkpoint`` is true (or the Checkpoint to write), else None."""
     code = _kind(kind)
     device = _device_of(a, "a")
-    ma = _matrix(a, "a")
-    if code == 1 and ma.cols % 2:
+    handle = _here(device, stream)
+    if handle is None:
+        with _switched(device, stream):
+            return lionmuon_activation(a, kind, out, checkpoint)
+    m = _matrix(a, "a", device)
+    rows, cols = m.rows, m.cols
+    if code == 1 and cols % 2:
         _invalid("a must have an even number of columns")
-    with _stream(device, stream) as handle:
-        if out is None:
-            out = torch.empty(ma.rows, ma.cols // (1 + code), dtype=a.dtype, device=device)
-        kept = _wanted(checkpoint, ma.rows, ma.cols, device)
-        mk = None if kept is None else _codes(kept, "checkpoint", device)
-        _done(_lib().lionmuon_activation(ma, code, _matrix(out, "out", device), _ref(mk), handle),
-              "lionmuon_activation")
+    if out is None:
+        out, mo = _new(rows, cols // (1 + code), a, m.dtype)
+    else:
+        mo = _matrix(out, "out", device)
+    kept = _wanted(checkpoint, rows, cols, device)
+    _done(_lib().lionmuon_activation(m, code, mo, None if kept is None else kept._desc, handle),
+          "lionmuon_activation")
     return out, kept
-
-
-def _wanted(checkpoint, rows, cols, device):
-    if isinstance(checkpoint, Checkpoint):
-        return checkpoint
-    return Checkpoint.empty(rows, cols, device) if checkpoint else None
 
 
 def lionmuon_activation_grad(dh, a, kind, out=None, recompute=False, stream=None):
@@ -309,19 +341,29 @@ def lionmuon_activation_grad(dh, a, kind, out=None, recompute=False, stream=None
     true (or the tensor to write), else None."""
     code = _kind(kind)
     device = _device_of(dh, "dh")
-    md = _matrix(dh, "dh")
-    kept = isinstance(a, Checkpoint)
-    ma = None if kept else _matrix(a, "a", device)
-    mk = _codes(a, "a", device) if kept else None
-    with _stream(device, stream) as handle:
-        if out is None:
-            out = torch.empty(md.rows, md.cols * (1 + code), dtype=dh.dtype, device=device)
-        h = recompute if isinstance(recompute, torch.Tensor) else \
-            torch.empty(md.rows, md.cols, dtype=dh.dtype, device=device) if recompute else None
-        mh = None if h is None else _matrix(h, "recompute", device)
-        _done(_lib().lionmuon_activation_grad(md, _ref(ma), _ref(mk), code,
-                                              _matrix(out, "out", device), _ref(mh), handle),
-              "lionmuon_activation_grad")
+    handle = _here(device, stream)
+    if handle is None:
+        with _switched(device, stream):
+            return lionmuon_activation_grad(dh, a, kind, out, recompute)
+    m = _matrix(dh, "dh", device)
+    rows, cols = m.rows, m.cols
+    ma = mk = None
+    if isinstance(a, Checkpoint):
+        mk = _codes(a, "a", device)
+    else:
+        ma = _matrix(a, "a", device)
+    if out is None:
+        out, mo = _new(rows, cols * (1 + code), dh, m.dtype)
+    else:
+        mo = _matrix(out, "out", device)
+    if isinstance(recompute, torch.Tensor):
+        h, mh = recompute, _matrix(recompute, "recompute", device)
+    elif recompute:
+        h, mh = _new(rows, cols, dh, m.dtype)
+    else:
+        h = mh = None
+    _done(_lib().lionmuon_activation_grad(m, ma, mk, code, mo, mh, handle),
+          "lionmuon_activation_grad")
     return out, h
 
 
@@ -335,25 +377,33 @@ def lionmuon_rmsnorm(x, weight, residual=None, eps=1e-5, out=None, sum_out=None,
     ``residual``); kept is the 8-bit checkpoint of y if ``checkpoint`` is true
     (or the Checkpoint to write), else None."""
     device = _device_of(x, "x")
-    mx = _matrix(x, "x")
-    mr = None if residual is None else _matrix(residual, "residual", device)
-    if sum_out is not None and residual is None:
+    handle = _here(device, stream)
+    if handle is None:
+        with _switched(device, stream):
+            return lionmuon_rmsnorm(x, weight, residual, eps, out, sum_out, checkpoint)
+    m = _matrix(x, "x", device)
+    rows, cols = m.rows, m.cols
+    w = _vector(weight, cols, "weight", device)
+    s, mr, ms = x, None, None
+    if residual is not None:
+        mr = _matrix(residual, "residual", device)
+        if sum_out is None:
+            s, ms = _new(rows, cols, x, m.dtype)
+        else:
+            s, ms = sum_out, _matrix(sum_out, "sum_out", device)
+    elif sum_out is not None:
         _invalid("sum_out needs a residual")
-    w = _vector(weight, mx.cols, "weight", device)
-    with _stream(device, stream) as handle:
-        y = None if out is False else torch.empty_like(x, memory_format=torch.contiguous_format) \
-            if out is None else out
-        my = None if y is None else _matrix(y, "out", device)
-        s, ms = x, None
-        if residual is not None:
-            s = torch.empty_like(x, memory_format=torch.contiguous_format) if sum_out is None \
-                else sum_out
-            ms = _matrix(s, "sum_out", device)
-        rstd = torch.empty(mx.rows, dtype=torch.float32, device=device)
-        kept = _wanted(checkpoint, mx.rows, mx.cols, device)
-        mk = None if kept is None else _codes(kept, "checkpoint", device)
-        _done(_lib().lionmuon_rmsnorm(mx, _ref(mr), w, eps, _ref(my), _ref(ms), rstd.data_ptr(),
-                                      _ref(mk), handle), "lionmuon_rmsnorm")
+    if out is None:
+        y, my = _new(rows, cols, x, m.dtype)
+    elif out is False:
+        y = my = None
+    else:
+        y, my = out, _matrix(out, "out", device)
+    rstd = torch.empty(rows, dtype=torch.float32, device=device)
+    kept = _wanted(checkpoint, rows, cols, device)
+    _done(_lib().lionmuon_rmsnorm(m, mr, w, eps, my, ms, rstd.data_ptr(),
+                                  None if kept is None else kept._desc, handle),
+          "lionmuon_rmsnorm")
     return y, s, rstd, kept
 
 
@@ -365,38 +415,49 @@ def lionmuon_rmsnorm_grad(dy, s, weight, rstd, residual_grad=None, out=None, wei
     dweight is float32, written to ``weight_grad`` (added to it with
     ``accumulate``). ``weight_grad=False`` or ``out=False`` leaves one out (None)."""
     device = _device_of(dy, "dy")
-    md = _matrix(dy, "dy")
-    kept = isinstance(s, Checkpoint)
-    ms = None if kept else _matrix(s, "s", device)
-    mk = _codes(s, "s", device) if kept else None
+    handle = _here(device, stream)
+    if handle is None:
+        with _switched(device, stream):
+            return lionmuon_rmsnorm_grad(dy, s, weight, rstd, residual_grad, out, weight_grad,
+                                         accumulate)
+    m = _matrix(dy, "dy", device)
+    rows, cols = m.rows, m.cols
+    ms = mk = None
+    if isinstance(s, Checkpoint):
+        mk = _codes(s, "s", device)
+    else:
+        ms = _matrix(s, "s", device)
     mr = None if residual_grad is None else _matrix(residual_grad, "residual_grad", device)
-    w = _vector(weight, md.cols, "weight", device)
-    r = _vector(rstd, md.rows, "rstd", device)
-    lib = _lib()
+    w = _vector(weight, cols, "weight", device)
+    r = _vector(rstd, rows, "rstd", device)
     if accumulate and not isinstance(weight_grad, torch.Tensor):
         _invalid("accumulate needs weight_grad")
-    with _stream(device, stream) as handle:
-        dx = None if out is False else torch.empty_like(dy, memory_format=torch.contiguous_format) \
-            if out is None else out
-        mdx = None if dx is None else _matrix(dx, "out", device)
-        dw, ws, nbytes = None, None, 0
-        if weight_grad is not False:
-            dw = torch.empty(md.cols, dtype=torch.float32, device=device) if weight_grad is None \
-                else weight_grad
-            nbytes = lionmuon_rmsnorm_workspace_bytes(md.rows, md.cols)
-            if nbytes:
-                ws = torch.empty(nbytes, dtype=torch.uint8, device=device)
-        pw = None if dw is None else _vector(dw, md.cols, "weight_grad", device)
-        _done(lib.lionmuon_rmsnorm_grad(md, _ref(ms), _ref(mk), w, r, _ref(mr), _ref(mdx), pw,
-                                        1 if accumulate else 0,
-                                        None if ws is None else ws.data_ptr(), nbytes, handle),
-              "lionmuon_rmsnorm_grad")
+    if out is None:
+        dx, mdx = _new(rows, cols, dy, m.dtype)
+    elif out is False:
+        dx = mdx = None
+    else:
+        dx, mdx = out, _matrix(out, "out", device)
+    dw = pw = ws = None
+    nbytes = 0
+    if weight_grad is not False:
+        if weight_grad is None:
+            dw = torch.empty(cols, dtype=torch.float32, device=device)
+            pw = dw.data_ptr()
+        else:
+            dw, pw = weight_grad, _vector(weight_grad, cols, "weight_grad", device)
+        nbytes = lionmuon_rmsnorm_workspace_bytes(rows, cols)
+        if nbytes:
+            ws = torch.empty(nbytes, dtype=torch.uint8, device=device)
+    _done(_lib().lionmuon_rmsnorm_grad(m, ms, mk, w, r, mr, mdx, pw, 1 if accumulate else 0,
+                                       None if ws is None else ws.data_ptr(), nbytes, handle),
+          "lionmuon_rmsnorm_grad")
     return dx, dw
 
 
 def lionmuon_rmsnorm_workspace_bytes(rows, cols) -> int:
     out = ctypes.c_size_t(0)
-    _done(_lib().lionmuon_rmsnorm_workspace_bytes(rows, cols, ctypes.byref(out)),
+    _done(_lib().lionmuon_rmsnorm_workspace_bytes(rows, cols, out),
           "lionmuon_rmsnorm_workspace_bytes")
     return out.value
 
@@ -408,28 +469,36 @@ def lionmuon_grouped_product(x, w, offsets, out=None, stream=None):
     tensor of experts + 1 values. Rows of no expert keep what ``out`` holds
     (a new ``out`` is not initialised there)."""
     device = _device_of(x, "x")
-    mx = _matrix(x, "x")
+    handle = _here(device, stream)
+    if handle is None:
+        with _switched(device, stream):
+            return lionmuon_grouped_product(x, w, offsets, out)
+    m = _matrix(x, "x", device)
     mw = _stack(w, "w", device)
     at = _offsets(offsets, mw.count, device)
-    with _stream(device, stream) as handle:
-        if out is None:
-            out = torch.empty(mx.rows, mw.rows, dtype=x.dtype, device=device)
-        _done(_lib().lionmuon_grouped_product(mx, mw, at, _matrix(out, "out", device), handle),
-              "lionmuon_grouped_product")
+    if out is None:
+        out, mo = _new(m.rows, mw.rows, x, m.dtype)
+    else:
+        mo = _matrix(out, "out", device)
+    _done(_lib().lionmuon_grouped_product(m, mw, at, mo, handle), "lionmuon_grouped_product")
     return out
 
 
 def lionmuon_grouped_input_grad(dy, w, offsets, out=None, stream=None):
     """dX[r] = dY[r] W_e (see lionmuon_grouped_product). dy: (T, n)."""
     device = _device_of(dy, "dy")
-    md = _matrix(dy, "dy")
+    handle = _here(device, stream)
+    if handle is None:
+        with _switched(device, stream):
+            return lionmuon_grouped_input_grad(dy, w, offsets, out)
+    m = _matrix(dy, "dy", device)
     mw = _stack(w, "w", device)
     at = _offsets(offsets, mw.count, device)
-    with _stream(device, stream) as handle:
-        if out is None:
-            out = torch.empty(md.rows, mw.cols, dtype=dy.dtype, device=device)
-        _done(_lib().lionmuon_grouped_input_grad(md, mw, at, _matrix(out, "out", device), handle),
-              "lionmuon_grouped_input_grad")
+    if out is None:
+        out, mo = _new(m.rows, mw.cols, dy, m.dtype)
+    else:
+        mo = _matrix(out, "out", device)
+    _done(_lib().lionmuon_grouped_input_grad(m, mw, at, mo, handle), "lionmuon_grouped_input_grad")
     return out
 
 
@@ -438,32 +507,41 @@ def lionmuon_grouped_weight_grad(dy, x, offsets, out=None, accumulate=False, str
     ``accumulate``. ``x``: (T, k) tensor of dy's type or its Checkpoint (dy must then
     be bfloat16). ``out.unbind()`` are gradients as the step takes them."""
     device = _device_of(dy, "dy")
-    md = _matrix(dy, "dy")
-    kept = isinstance(x, Checkpoint)
-    mx = None if kept else _matrix(x, "x", device)
-    mk = _codes(x, "x", device) if kept else None
-    cols = (mk or mx).cols
-    if not isinstance(offsets, torch.Tensor):
-        raise TypeError("offsets must be a torch.Tensor")
-    if accumulate and out is None:
-        _invalid("accumulate needs out")
-    experts = offsets.numel() - 1 if out is None else out.shape[0]
-    at = _offsets(offsets, experts, device)
-    with _stream(device, stream) as handle:
-        if out is None:
-            out = torch.empty(experts, md.cols, cols, dtype=torch.float32, device=device)
-        mo = _stack(out, "out", device)
-        nbytes = lionmuon_grouped_workspace_bytes(md.rows, experts, md.cols, cols)
-        ws = torch.empty(nbytes, dtype=torch.uint8, device=device) if nbytes else None
-        _done(_lib().lionmuon_grouped_weight_grad(md, _ref(mx), _ref(mk), at, mo,
-                                                  1 if accumulate else 0,
-                                                  None if ws is None else ws.data_ptr(), nbytes,
-                                                  handle), "lionmuon_grouped_weight_grad")
+    handle = _here(device, stream)
+    if handle is None:
+        with _switched(device, stream):
+            return lionmuon_grouped_weight_grad(dy, x, offsets, out, accumulate)
+    m = _matrix(dy, "dy", device)
+    mx = mk = None
+    if isinstance(x, Checkpoint):
+        mk = _codes(x, "x", device)
+        cols = mk.cols
+    else:
+        mx = _matrix(x, "x", device)
+        cols = mx.cols
+    if out is None:
+        if accumulate:
+            _invalid("accumulate needs out")
+        _check_place(offsets, "offsets", device)
+        experts = offsets.numel() - 1
+        at = _offsets(offsets, experts, device)
+        out = torch.empty((experts, m.cols, cols), dtype=torch.float32, device=device)
+    else:
+        experts = None
+    mo = _stack(out, "out", device)
+    if experts is None:
+        experts = mo.count
+        at = _offsets(offsets, experts, device)
+    nbytes = lionmuon_grouped_workspace_bytes(m.rows, experts, m.cols, cols)
+    ws = torch.empty(nbytes, dtype=torch.uint8, device=device) if nbytes else None
+    _done(_lib().lionmuon_grouped_weight_grad(m, mx, mk, at, mo, 1 if accumulate else 0,
+                                              None if ws is None else ws.data_ptr(), nbytes,
+                                              handle), "lionmuon_grouped_weight_grad")
     return out
 
 
 def lionmuon_grouped_workspace_bytes(rows, experts, n, k) -> int:
     out = ctypes.c_size_t(0)
-    _done(_lib().lionmuon_grouped_workspace_bytes(rows, experts, n, k, ctypes.byref(out)),
+    _done(_lib().lionmuon_grouped_workspace_bytes(rows, experts, n, k, out),
           "lionmuon_grouped_workspace_bytes")
     return out.value
