@@ -65,52 +65,69 @@ __device__ __forceinline__ u32x4 descriptor(const void* p, int64_t bytes) {
 }
 constexpr uint32_t kOutside = 0x80000000u;   // beyond every descriptor
 
-// 16 bytes a lane from the buffer to LDS: lane i's land at dst + 16 i. The
+// 16 bytes a lane from the buffer to LDS: lane i's land at address dst + 16 i. The
 // compiler neither counts these copies nor waits for them: every wait for them is
 // explicit. (An assembly block without outputs: nothing the compiler could
 // reuse while the copy is in flight.)
-__device__ __forceinline__ void copy16(u32x4 desc, uint32_t off, const void* dst) {
-  const uint32_t d = uint32_t(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) const char*)(dst)));
+__device__ __forceinline__ void copy16(u32x4 desc, uint32_t off, uint32_t dst) {
   const u32x4 u = {uint32_t(__builtin_amdgcn_readfirstlane(desc[0])), uint32_t(__builtin_amdgcn_readfirstlane(desc[1])),
                    uint32_t(__builtin_amdgcn_readfirstlane(desc[2])), 0x00027000u};
   asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds"
-               :: "v"(off), "s"(u), "s"(__builtin_amdgcn_readfirstlane(d)) : "memory", "m0");
+               :: "v"(off), "s"(u), "s"(__builtin_amdgcn_readfirstlane(dst)) : "memory", "m0");
+}
+__device__ __forceinline__ uint32_t lds_address(const void* p) {
+  return uint32_t(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) const char*)(p)));
 }
 
-// Expert and first row of row tile `slot` (BM rows each). Expert e's tiles
-// start at slot floor(offsets[e] / BM) + e: its ceil(rows / BM) tiles end at or
-// before the next expert's first slot, whatever the offsets, so that T / BM + count
-// slots hold every tile and one look at the offsets finds a slot's expert: the last
-// one whose first slot is not behind it. Offsets are clamped to [0, rows], so wrong
-// ones cannot lead outside. Returns false for a slot without rows.
-__device__ __forceinline__ bool find_slot(const int32_t* offsets, int experts, int rows, int bm, int slot, int* expert, int* index) {
-  const int lane = threadIdx.x & 63;
-  int e = -1;
-  for (int base = 0; base < experts; base += 64) {
-    const int i = base + lane;
-    const int off = min(max(offsets[min(i, experts - 1)], 0), rows);
-    const uint64_t m = __ballot(i < experts && off / bm + i <= slot);
-    if (m == 0) break;
-    e = base + 63 - __builtin_clzll(m);
-  }
-  e = __builtin_amdgcn_readfirstlane(e);
-  if (e < 0) return false;
-  *expert = e;
-  *index = __builtin_amdgcn_readfirstlane(slot - (min(max(offsets[e], 0), rows) / bm + e));
-  return true;
-}
-
-struct RowTile {
-  int expert, row0, end;
+// Groups of `bm` rows that each expert makes (at least `least`), counted through
+// the experts. The host knows the total of rows only; a wave counts 64 experts at a
+// time. Offsets are clamped to [0, rows], so wrong ones cannot lead outside.
+struct Span {
+  int expert, index, row0, end;      // row0: of the expert's group `index`
 };
-template <int BM>
-__device__ __forceinline__ bool find_tile(const int32_t* offsets, int experts, int rows, int slot, RowTile* t) {
-  int e, i;
-  if (!find_slot(offsets, experts, rows, BM, slot, &e, &i)) return false;
-  t->expert = e;
-  t->row0 = __builtin_amdgcn_readfirstlane(min(max(offsets[e], 0), rows) + i * BM);
-  t->end = __builtin_amdgcn_readfirstlane(min(max(offsets[e + 1], 0), rows));
-  return t->row0 < t->end;
+__device__ __forceinline__ int groups_of(const int32_t* offsets, int experts, int rows, int bm, int least, int i, int* first, int* end) {
+  const int j = min(i, experts - 1);
+  *first = min(max(offsets[j], 0), rows);
+  *end = min(max(offsets[j + 1], 0), rows);
+  return i < experts ? max((max(*end - *first, 0) + bm - 1) / bm, least) : 0;
+}
+__device__ __forceinline__ int wave_scan(int v, int lane) {      // inclusive
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const int up = __shfl_up(v, d, 64);
+    v += lane >= d ? up : 0;
+  }
+  return v;
+}
+__device__ __forceinline__ int count_groups(const int32_t* offsets, int experts, int rows, int bm, int least) {
+  const int lane = threadIdx.x & 63;
+  int total = 0;
+  for (int base = 0; base < experts; base += 64) {
+    int first, end;
+    const int n = groups_of(offsets, experts, rows, bm, least, base + lane, &first, &end);
+    total += __builtin_amdgcn_readlane(wave_scan(n, lane), 63);
+  }
+  return total;
+}
+// Group `id` (below the count).
+__device__ __forceinline__ Span find_group(const int32_t* offsets, int experts, int rows, int bm, int least, int id) {
+  const int lane = threadIdx.x & 63;
+  Span t{0, 0, 0, 0};
+  for (int base = 0; base < experts; base += 64) {
+    int first, end;
+    const int n = groups_of(offsets, experts, rows, bm, least, base + lane, &first, &end);
+    const int upto = wave_scan(n, lane), here = __builtin_amdgcn_readlane(upto, 63);
+    if (id < here) {
+      const int l = __builtin_ctzll(__ballot(upto > id));
+      t.expert = base + l;
+      t.index = id - (__builtin_amdgcn_readlane(upto, l) - __builtin_amdgcn_readlane(n, l));
+      t.row0 = __builtin_amdgcn_readlane(first, l) + t.index * bm;
+      t.end = __builtin_amdgcn_readlane(end, l);
+      break;
+    }
+    id -= here;
+  }
+  return t;
 }
 
 enum { kRows = 0, kCols = 1, kCodes = 2 };   // operand: along, across, across in 8 bits
@@ -147,18 +164,18 @@ __device__ __forceinline__ void banded(int id, int m, int n, int* i, int* j) {
   *i = first + r - *j * h;
 }
 
-// One operand's stage of 64 contraction values by a tile of W rows or columns.
+// One operand's stage of KS contraction values by a tile of W rows or columns.
 // Chunk c (16 bytes) of the stage, in the order that LDS holds them, is taken by
 // copy instruction c / 64, lane c % 64.
-template <int MODE, int W>
+template <int MODE, int W, int KS>
 struct Stage {
-  static constexpr int kChunks = W * 8;                       // of 16 bytes
-  static constexpr int kPerRow = MODE == kRows ? 8 : W / 8;   // chunks of an LDS row
+  static constexpr int kChunks = W * KS / 8;                        // of 16 bytes
+  static constexpr int kPerRow = MODE == kRows ? KS / 8 : W / 8;    // chunks of an LDS row
   // Physical chunk of logical chunk c in LDS row r is c ^ swz(r): 16 rows of a
   // fragment read (kRows), or the four rows of a transpose read (kCols), fall into
   // different banks. (Rows of 64 columns are 8 chunks: there rows go in pairs.)
   __device__ static __forceinline__ int swz(int r) {
-    if (MODE == kRows) return (r & 7) ^ ((r >> 3) & 1);
+    if (MODE == kRows) return kPerRow == 4 ? (r >> 2) & 3 : (r & 7) ^ ((r >> 3) & 1);
     return kPerRow == 8 ? ((r >> 1) & 1) * 4 : (r & 3) * 4;
   }
   __device__ static __forceinline__ void place(int c, int* row, int* chunk) {
@@ -177,23 +194,30 @@ struct Source {
   bool wide;            // the matrix's rows hold at least eight elements
 };
 
-// DA, DB: the operand goes straight to LDS, else through registers.
-template <typename T, int MA, int MB, int BM, int BN, int WM, int WN, int NB, bool DA, bool DB>
-struct Tile {
+// KS: contraction values of a stage; NB: stages in LDS; SUB: groups of 16 values of
+// a step (below); DA, DB: the operand goes straight to LDS, else through registers.
+template <int BM_, int BN_, int WM_, int WN_, int KS_, int NB_, int SUB_>
+struct Shape {
+  static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, KS = KS_, NB = NB_, SUB = SUB_;
   static constexpr int kWavesN = BN / WN, kWaves = (BM / WM) * kWavesN, kThreads = kWaves * 64;
+  static constexpr int kWorkgroups = BM * BN <= 128 * 128 ? 2 : 1;      // on a CU at least
+};
+
+template <typename T, int MA, int MB, class S, bool DA, bool DB>
+struct Tile {
+  static constexpr int BM = S::BM, BN = S::BN, WM = S::WM, WN = S::WN, KS = S::KS, NB = S::NB, SUB = S::SUB;
+  static constexpr int kWavesN = S::kWavesN, kWaves = S::kWaves, kThreads = S::kThreads;
   static constexpr int kMI = WM / 32, kNI = WN / 32;
-  static constexpr int kStageBytes = (BM + BN) * 128;
-  static constexpr int kLds = NB * kStageBytes;      // NB stages
-  using SA = Stage<MA, BM>;
-  using SB = Stage<MB, BN>;
+  static constexpr int kStageA = BM * KS * 2, kStageBytes = (BM + BN) * KS * 2;
+  static constexpr int kLds = NB * kStageBytes;
 
   // Copies of one operand's stages (16-bit operands), by DMA: kInst copies of a
   // wave for each stage of 64 contraction values.
   template <int MODE, int W>
   struct Copier {
-    using S = Stage<MODE, W>;
-    static constexpr int kInst = S::kChunks / 64 / kWaves, kStepRows = 64 * kWaves / S::kPerRow;
-    static_assert(kInst * 64 * kWaves == S::kChunks, "whole copies");
+    using G = Stage<MODE, W, KS>;
+    static constexpr int kInst = G::kChunks / 64 / kWaves, kStepRows = 64 * kWaves / G::kPerRow;
+    static_assert(kInst * 64 * kWaves == G::kChunks, "whole copies");
     static_assert(MODE == kRows ? kStepRows % 16 == 0 : kStepRows % 4 == 0, "one swizzle for all copies of a lane");
     Source s;
     uint32_t off;      // the lane's byte offset in the first copy
@@ -202,7 +226,7 @@ struct Tile {
     uint32_t at;
     __device__ __forceinline__ Copier(const Source& src, int wave, int lane) : s(src) {
       int row, chunk;
-      S::place(wave * 64 + lane, &row, &chunk);
+      G::place(wave * 64 + lane, &row, &chunk);
       off = uint32_t(row) * uint32_t(s.ld) + chunk * 16;
       first = chunk * 8;
     }
@@ -213,12 +237,12 @@ struct Tile {
         d = descriptor(s.p + int64_t(k0) * 2, s.rows > 0 ? (s.rows - 1) * s.ld + int64_t(s.depth - k0) * 2 : 0);
         if (k0 + first >= s.depth) at = kOutside;
       } else {
-        const int left = min(s.depth - k0, 64);
+        const int left = min(s.depth - k0, KS);
         d = descriptor(s.p + int64_t(k0) * s.ld, left > 0 ? (left - 1) * s.ld + int64_t(s.cols) * 2 : 0);
       }
     }
-    __device__ __forceinline__ void copy(int q, char* dst, int wave) const {
-      copy16(d, at + uint32_t(q * kStepRows) * uint32_t(s.ld), dst + (q * kWaves + wave) * 1024);
+    __device__ __forceinline__ void copy(int q, uint32_t dst) const {      // dst: LDS address of the wave's first copy
+      copy16(d, at + uint32_t(q * kStepRows) * uint32_t(s.ld), dst + q * kWaves * 1024);
     }
   };
 
@@ -228,14 +252,14 @@ struct Tile {
   // LDS, so that no load waits in a branch of its own.
   template <int MODE, int W>
   struct Regs {
-    static constexpr int kInst = Stage<MODE, W>::kChunks / kThreads;
+    static constexpr int kInst = Stage<MODE, W, KS>::kChunks / kThreads;
     u32x4 v[kInst];
   };
   // Elements of chunk q of a thread that exist (at most 8; 0: none).
   template <int MODE, int W>
   __device__ static __forceinline__ int present(const Source& s, int k0, int q, int tid, int* row, int* first) {
     int chunk;
-    Stage<MODE, W>::place(q * kThreads + tid, row, &chunk);
+    Stage<MODE, W, KS>::place(q * kThreads + tid, row, &chunk);
     *first = chunk * 8;
     const int n = (MODE == kRows ? s.depth - k0 : s.cols) - *first;
     const bool in = *row < (MODE == kRows ? s.rows : s.depth - k0);
@@ -273,7 +297,7 @@ struct Tile {
   }
   template <int MODE, int W>
   __device__ static __forceinline__ void put(const Source& s, int k0, const Regs<MODE, W>& r, int q, char* dst, int tid) {
-    const bool cut = MODE == kRows ? s.depth - k0 < 64 && s.depth % 8 != 0 : s.cols < W && s.cols % 8 != 0;
+    const bool cut = MODE == kRows ? s.depth - k0 < KS && s.depth % 8 != 0 : s.cols < W && s.cols % 8 != 0;
     int row, first;
     const int n = present<MODE, W>(s, k0, q, tid, &row, &first);
     u32x4 v = r.v[q];
@@ -290,7 +314,7 @@ struct Tile {
   // A checkpoint's stage: 16 codes a load, widened to bf16 (exactly: the scale
   // is a power of two) on the way into LDS.
   struct CodeRegs {
-    static constexpr int kInst = BN * 64 / 16 / kThreads;
+    static constexpr int kInst = BN * KS / 16 / kThreads;
     u32x4 v[kInst];
     uint32_t s[kInst];
   };
@@ -326,24 +350,24 @@ struct Tile {
       o[2 * w] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(r.v[q][2 * h + w], scale, false));
       o[2 * w + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(r.v[q][2 * h + w], scale, true));
     }
-    *reinterpret_cast<u32x4*>(dst + row * (BN * 2) + (c ^ SB::swz(row)) * 16) = o;
+    *reinterpret_cast<u32x4*>(dst + row * (BN * 2) + (c ^ Stage<kCols, BN, KS>::swz(row)) * 16) = o;
   }
 
   // Fragment of 32 rows (or columns) from `w0` on and contraction values
-  // 16 kk .. + 15: lane l holds row l % 32, values 8 (l / 32) .. + 7.
+  // 16 kk .. + 15 of a stage: lane l holds row l % 32, values 8 (l / 32) .. + 7.
   template <int MODE, int W>
   __device__ static __forceinline__ s16x8 fragment(const char* st, int w0, int kk, int lane) {
-    using S = Stage<MODE, W>;
+    using G = Stage<MODE, W, KS>;
     if constexpr (MODE == kRows) {
       const int r = w0 + (lane & 31);
-      return *reinterpret_cast<const s16x8*>(st + r * 128 + ((kk * 2 + (lane >> 5)) ^ S::swz(r)) * 16);
+      return *reinterpret_cast<const s16x8*>(st + r * (KS * 2) + ((kk * 2 + (lane >> 5)) ^ G::swz(r)) * 16);
     } else {
       // two transpose reads of four contraction values each: within 16 lanes
       // lane m points at row m / 4, columns 4 (m % 4) .. + 3, and gets column m of
       // those four rows
       const int g = lane >> 4, m = lane & 15;
       const int n = w0 + 16 * (g & 1) + 4 * (m & 3), k = kk * 16 + 8 * (g >> 1) + (m >> 2);
-      const char* p = st + k * (W * 2) + (((n >> 3) ^ S::swz(k)) * 16) + (n & 7) * 2;
+      const char* p = st + k * (W * 2) + (((n >> 3) ^ G::swz(k)) * 16) + (n & 7) * 2;
       typedef __attribute__((address_space(3))) s16x4 lds4;
       const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)(p));
       const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)(p + 4 * (W * 2)));
@@ -356,18 +380,18 @@ struct Tile {
   // matrix unit truncates where it adds to an accumulator, which long chains show;
   // vector additions round).
   //
-  // A stage is four steps of 16 values. The fragments of a step are read while the
-  // step before is multiplied, across stages too: one barrier a stage, before its
+  // A stage is kSteps steps of 16 SUB values. The fragments of a step are read while
+  // the step before is multiplied, across stages too: one barrier a stage, before its
   // last step, says that every wave has read the stage (its buffer takes the stage NB
-  // later) and that the next one has landed. Copies and fragment reads are
-  // placed one behind each MFMA, so that the matrix unit never waits for a batch of
-  // them, and so are the writes of what comes through registers.
+  // later) and that the next one has landed. Copies, fragment reads and the
+  // writes of what comes through registers are spread over the MFMAs, so that the matrix
+  // unit never waits for a batch of them to issue.
   template <int FOLD>
   __device__ static __forceinline__ void product(const Source& a, const Source& b, const CodeSource& c, int depth, char* smem, f32x16 (&out)[kMI][kNI]) {
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wm = (wave / kWavesN) * WM, wn = (wave % kWavesN) * WN;
-    const int nk = (depth + 63) / 64;
+    const int nk = (depth + KS - 1) / KS;
     constexpr int kModeB = MB == kCodes ? int(kCols) : MB;
     static_assert(!(DB && MB == kCodes), "codes go through registers");
     constexpr int kCopiesA = DA ? Copier<MA, BM>::kInst : 0, kCopiesB = DB ? Copier<kModeB, BN>::kInst : 0;
@@ -380,36 +404,37 @@ struct Tile {
     CodeRegs rc;
     // stages that go through registers: loaded one stage ahead of the write to LDS
     auto load = [&](int kt) {
-      if constexpr (!DA) fetch<MA, BM>(a, kt * 64, tid, ra);
-      if constexpr (!DB && MB != kCodes) fetch<kModeB, BN>(b, kt * 64, tid, rb);
+      if constexpr (!DA) fetch<MA, BM>(a, kt * KS, tid, ra);
+      if constexpr (!DB && MB != kCodes) fetch<kModeB, BN>(b, kt * KS, tid, rb);
     };
     auto load_codes = [&](int kt) {
-      if constexpr (MB == kCodes) fetch(c, kt * 64, tid, rc);
+      if constexpr (MB == kCodes) fetch(c, kt * KS, tid, rc);
     };
     constexpr int kWritesA = DA ? 0 : Regs<MA, BM>::kInst, kWritesB = (DB || MB == kCodes) ? 0 : Regs<kModeB, BN>::kInst;
     constexpr int kWrites = kWritesA + kWritesB;
     auto write = [&](int kt, int q, char* buf) {
       if constexpr (!DA) {
         if (q < kWritesA) {
-          put<MA, BM>(a, kt * 64, ra, q, buf, tid);
+          put<MA, BM>(a, kt * KS, ra, q, buf, tid);
           return;
         }
       }
-      if constexpr (!DB && MB != kCodes) put<kModeB, BN>(b, kt * 64, rb, q - kWritesA, buf + BM * 128, tid);
+      if constexpr (!DB && MB != kCodes) put<kModeB, BN>(b, kt * KS, rb, q - kWritesA, buf + kStageA, tid);
     };
-    auto widen = [&](int piece, char* buf) { put(rc, piece, buf + BM * 128, tid); };
+    auto widen = [&](int piece, char* buf) { put(rc, piece, buf + kStageA, tid); };
     auto start = [&](int kt) {
-      if constexpr (DA) ca.start(kt * 64);
-      if constexpr (DB) cb.start(kt * 64);
+      if constexpr (DA) ca.start(kt * KS);
+      if constexpr (DB) cb.start(kt * KS);
     };
-    auto copy = [&](int q, char* buf) {
+    const uint32_t lds = lds_address(smem) + wave * 1024;
+    auto copy = [&](int q, int buf) {              // buf: byte offset of a stage's buffer
       if constexpr (DA) {
         if (q < kCopiesA) {
-          ca.copy(q, buf, wave);
+          ca.copy(q, lds + buf);
           return;
         }
       }
-      if constexpr (DB) cb.copy(q - kCopiesA, buf + BM * 128, wave);
+      if constexpr (DB) cb.copy(q - kCopiesA, lds + buf + kStageA);
     };
     f32x16 acc[FOLD ? kMI : 1][FOLD ? kNI : 1];
     auto zero = [](auto& x) {
@@ -418,101 +443,134 @@ struct Tile {
     };
     zero(out);
     if (nk == 0) return;
+    constexpr int kSteps = KS / 16 / SUB, kFrags = SUB * (kMI + kNI), kMfmas = SUB * kMI * kNI;
+    // A stage's copies start in the last step of stage kt - NB, and, with more than
+    // two buffers, which leave them time to land, go on through that of the next
+    // stage's other steps: kFirst of them in the last step.
+    constexpr int kFirst = NB == 2 || kSteps == 1 ? kCopies : (kCopies + kSteps - 1) / kSteps;
     // (past the end copies read nothing and put zeros into a buffer that is not
     // read again: the number of copies in flight is always the same, and no
     // branch cuts the block of code that `step` orders)
 #pragma unroll
     for (int kt = 0; kt < NB; ++kt) {
-      char* buf = smem + kt * kStageBytes;
       start(kt);
 #pragma unroll
-      for (int q = 0; q < kCopies; ++q) copy(q, buf);
-      if (kt < nk) {
-        load(kt);
+      for (int q = 0; q < (kt + 1 < NB ? kCopies : kFirst); ++q) copy(q, kt * kStageBytes);
+    }
+    if constexpr (kWrites + kPiecesB > 0) {
+      for (int kt = 0; kt < NB; ++kt) {
+        char* to = smem + kt * kStageBytes;
+        if (kt < nk) {
+          load(kt);
 #pragma unroll
-        for (int q = 0; q < kWrites; ++q) write(kt, q, buf);
+          for (int q = 0; q < kWrites; ++q) write(kt, q, to);
+        }
+        load_codes(kt);
+#pragma unroll
+        for (int h = 0; h < kPiecesB; ++h) widen(h, to);
       }
-      load_codes(kt);
-#pragma unroll
-      for (int h = 0; h < kPiecesB; ++h) widen(h, buf);
     }
     if (NB < nk) load(NB);
     load_codes(NB);
-    wait_vmcnt<0>();
+    if constexpr (kCopies > 0) wait_vmcnt<(NB - 2) * kCopies + kFirst>();
     lds_barrier();
-    s16x8 fa[2][kMI], fb[2][kNI];
-    // fragment f of step kk (0..3) of the stage in `buf`: A's blocks, then B's
-    auto read = [&](int slot, const char* buf, int kk, int f) {
-      if (f < kMI) fa[slot][f] = fragment<MA, BM>(buf, wm + 32 * f, kk, lane);
-      else fb[slot][f - kMI] = fragment<kModeB, BN>(buf + BM * 128, wn + 32 * (f - kMI), kk, lane);
+    s16x8 fa[2][SUB * kMI], fb[2][SUB * kNI];
+    // fragment f of step st of the stage at buf: of each 16 values A's blocks, then B's
+    auto read = [&](int slot, int buf, int st, int f) {
+      const int u = f / (kMI + kNI), g = f % (kMI + kNI);
+      const char* p = smem + buf;
+      if (g < kMI) fa[slot][u * kMI + g] = fragment<MA, BM>(p, wm + 32 * g, st * SUB + u, lane);
+      else fb[slot][u * kNI + g - kMI] = fragment<kModeB, BN>(p + kStageA, wn + 32 * (g - kMI), st * SUB + u, lane);
     };
-    constexpr int kFrags = kMI + kNI, kMfmas = kMI * kNI;
 #pragma unroll
-    for (int f = 0; f < kFrags; ++f) read(0, smem, 0, f);
-    // one step: its MFMAs, each followed by its share of the next step's reads (step
-    // kk1 of the stage in `next`) and, in the last step, of what fills `fill`
-    auto step = [&](int kk, const char* next, int kk1, char* fill, int kt) {
-      const int cur = kk & 1, nxt = cur ^ 1;
+    for (int f = 0; f < kFrags; ++f) read(0, 0, 0, f);
+    // One step (fragments in slot `cur`): its MFMAs, each followed by its share of the
+    // next step's reads (step st1 of the stage at buf1), of copies q0 .. q1 to
+    // `fill` and, in the last step, of the writes to it.
+    auto step = [&](int cur, int buf1, int st1, int fill, int q0, int q1, bool last, int kt) {
 #pragma unroll
       for (int m = 0; m < kMfmas; ++m) {
-        const int i = m / kNI, j = m % kNI;
-        if constexpr (FOLD > 0) acc[i][j] = mma(fa[cur][i], fb[cur][j], acc[i][j], T());
-        else out[i][j] = mma(fa[cur][i], fb[cur][j], out[i][j], T());
+        const int u = m / (kMI * kNI), i = m / kNI % kMI, j = m % kNI;
+        if constexpr (FOLD > 0) acc[i][j] = mma(fa[cur][u * kMI + i], fb[cur][u * kNI + j], acc[i][j], T());
+        else out[i][j] = mma(fa[cur][u * kMI + i], fb[cur][u * kNI + j], out[i][j], T());
 #pragma unroll
-        for (int f = m * kFrags / kMfmas; f < (m + 1) * kFrags / kMfmas; ++f) read(nxt, next, kk1, f);
-        if (kk == 3) {
-          // what comes through registers first: the wait for it would include
-          // copies that have just been started
-          constexpr int kHalf = kPiecesB + kWrites == 0 ? 0 : kCopies == 0 || kMfmas == 1 ? kMfmas : kMfmas / 2;
-          constexpr int kParts = kHalf > 0 ? kHalf : 1;
-          if (m < kHalf) {
+        for (int f = m * kFrags / kMfmas; f < (m + 1) * kFrags / kMfmas; ++f) read(cur ^ 1, buf1, st1, f);
+        // what comes through registers first: the wait for it would include
+        // copies that have just been started
+        constexpr int kParts = kPiecesB + kWrites == 0 ? 0 : kCopies == 0 || kMfmas == 1 ? kMfmas : kMfmas / 2;
+        const bool regs = last && m < kParts;
+        if (regs) {
+          constexpr int kD = kParts > 0 ? kParts : 1;
 #pragma unroll
-            for (int h = m * kPiecesB / kParts; h < (m + 1) * kPiecesB / kParts; ++h) widen(h, fill);
+          for (int h = m * kPiecesB / kD; h < (m + 1) * kPiecesB / kD; ++h) widen(h, smem + fill);
 #pragma unroll
-            for (int q = m * kWrites / kParts; q < (m + 1) * kWrites / kParts; ++q) write(kt, q, fill);
-          }
-          if (m >= kHalf || kMfmas == 1) {
-            constexpr int kAt = kMfmas == 1 ? 0 : kHalf, kRest = kMfmas - kAt > 0 ? kMfmas - kAt : 1;
+          for (int q = m * kWrites / kD; q < (m + 1) * kWrites / kD; ++q) write(kt, q, smem + fill);
+        }
+        if (!regs || kMfmas == 1) {
+          const int at = last && kMfmas > 1 ? kParts : 0, n = q1 - q0;
 #pragma unroll
-            for (int q = (m - kAt) * kCopies / kRest; q < (m - kAt + 1) * kCopies / kRest; ++q) copy(q, fill);
-          }
+          for (int q = (m - at) * n / (kMfmas - at); q < (m - at + 1) * n / (kMfmas - at); ++q) copy(q0 + q, fill);
         }
         __builtin_amdgcn_sched_barrier(0);
       }
     };
-    char* buf = smem;
-    auto stage = [&](int kt) {
-      char* next = buf == smem + (NB - 1) * kStageBytes ? smem : buf + kStageBytes;
-      step(0, buf, 1, buf, 0);
-      step(1, buf, 2, buf, 0);
-      step(2, buf, 3, buf, 0);
+    int buf = 0, filling = (NB - 1) * kStageBytes;
+    auto stage = [&](int kt, int par) {
+      const int next = buf == (NB - 1) * kStageBytes ? 0 : buf + kStageBytes;
+#pragma unroll
+      for (int st = 0; st + 1 < kSteps; ++st) {
+        constexpr int kLeft = kCopies - kFirst, kOver = kSteps > 1 ? kSteps - 1 : 1;
+        step((par + st) & 1, buf, st + 1, filling, kFirst + st * kLeft / kOver, kFirst + (st + 1) * kLeft / kOver, false, 0);
+      }
       // stage kt + 1 has landed: at least that many copies of later ones
       // were started after its own
       if constexpr (kCopies > 0) wait_vmcnt<(NB - 2) * kCopies>();
       lds_barrier();
       start(kt + NB);
       __builtin_amdgcn_sched_barrier(0);
-      step(3, next, 0, buf, kt + NB);
+      step((par + kSteps - 1) & 1, next, 0, buf, 0, kFirst, true, kt + NB);
       // (the registers are free now)
       if (kt + NB + 1 < nk) load(kt + NB + 1);
       load_codes(kt + NB + 1);
       __builtin_amdgcn_sched_barrier(0);
+      filling = buf;
       buf = next;
+    };
+    // stages in [k0, k1), two at a time where a stage has an odd number of steps,
+    // so that the fragments' slots are known to the compiler
+    auto stages = [&](int k0, int k1) {
+      if constexpr (kSteps % 2 == 0) {
+#pragma unroll 1
+        for (int kt = k0; kt < k1; ++kt) stage(kt, 0);
+      } else {
+        // (an odd one out is a whole pair's first: the slots then start over, so its
+        // fragments move once)
+        int kt = k0;
+#pragma unroll 1
+        for (; kt + 2 <= k1; kt += 2) {
+          stage(kt, 0);
+          stage(kt + 1, 1);
+        }
+        if (kt < k1) {
+          stage(kt, 0);
+#pragma unroll
+          for (int f = 0; f < SUB * kMI; ++f) fa[0][f] = fa[1][f];
+#pragma unroll
+          for (int f = 0; f < SUB * kNI; ++f) fb[0][f] = fb[1][f];
+        }
+      }
     };
     if constexpr (FOLD > 0) {
       for (int k0 = 0; k0 < nk; k0 += FOLD) {
         zero(acc);
-        const int k1 = min(k0 + FOLD, nk);
-#pragma unroll 1
-        for (int kt = k0; kt < k1; ++kt) stage(kt);
+        stages(k0, min(k0 + FOLD, nk));
 #pragma unroll
         for (int i = 0; i < kMI; ++i)
 #pragma unroll
           for (int j = 0; j < kNI; ++j) out[i][j] += acc[i][j];
       }
     } else {
-#pragma unroll 1
-      for (int kt = 0; kt < nk; ++kt) stage(kt);
+      stages(0, nk);
     }
     wait_vmcnt<0>();
   }
@@ -529,22 +587,26 @@ struct RowProduct {
   int64_t lda, ldb, ldc, b_stride;    // elements
   int rows, experts;
   int width, depth;                   // columns of the output, contraction
-  int slots, tiles_n, chunk;
+  int tiles_n;
   int vec_out;                        // rows of the output start 16-byte aligned
 };
 
-template <typename T, int MB, int BM, int BN, int WM, int WN, int NB, bool DA, bool DB>
-__global__ __launch_bounds__((BM / WM) * (BN / WN) * 64, BM * BN <= 128 * 128 ? 2 : 1) void row_product_kernel(RowProduct g) {
-  using K = Tile<T, kRows, MB, BM, BN, WM, WN, NB, DA, DB>;
+template <typename T, int MB, class S, bool DA, bool DB>
+__global__ __launch_bounds__(S::kThreads, S::kWorkgroups) void row_product_kernel(RowProduct g) {
+  using K = Tile<T, kRows, MB, S, DA, DB>;
+  constexpr int BM = S::BM, BN = S::BN, WM = S::WM, WN = S::WN;
   constexpr int kStage = 32 * (WN + 8);         // elements of a wave's output staging
   static_assert(K::kWaves * kStage * 2 <= K::kLds, "staging fits");
   __shared__ __align__(16) char smem[K::kLds];
-  int slot, tn;
-  const int id = by_xcd(blockIdx.x, g.chunk);
-  if (id >= g.slots * g.tiles_n) return;
-  banded(id, g.slots, g.tiles_n, &slot, &tn);
-  RowTile t;
-  if (!find_tile<BM>(g.offsets, g.experts, g.rows, slot, &t)) return;
+  // An XCD (every eighth workgroup) takes an eighth of the tiles that there
+  // are, neighbours that share operands in its L2.
+  const int tiles_m = count_groups(g.offsets, g.experts, g.rows, BM, 0);
+  const int tiles = tiles_m * g.tiles_n, each = (tiles + 7) / 8, turn = blockIdx.x / 8;
+  const int id = int(blockIdx.x % 8) * each + turn;
+  if (turn >= each || id >= tiles) return;
+  int tm, tn;
+  banded(id, tiles_m, g.tiles_n, &tm, &tn);
+  const Span t = find_group(g.offsets, g.experts, g.rows, BM, 0, tm);
   const int col0 = tn * BN;
   const T* w = static_cast<const T*>(g.b) + t.expert * g.b_stride;
   Source a, b;
@@ -615,7 +677,6 @@ struct WeightProduct {
   int rows, experts, n, k;
   int tiles_m, tiles_n, chunk;
   int part;                           // rows of a part of an expert; > rows: whole experts
-  int units;
   int accumulate;
 };
 
@@ -626,28 +687,32 @@ struct WeightProduct {
 // and needs 2 rows / part + 1 in all.
 __device__ __forceinline__ int partial_slot(int first, int part) { return int(2 * int64_t(first) / part); }
 
-template <typename T, int MB, int BM, int BN, int WM, int WN, int NB, bool DA, bool DB>
-__global__ __launch_bounds__((BM / WM) * (BN / WN) * 64, BM * BN <= 128 * 128 ? 2 : 1) void weight_product_kernel(WeightProduct g) {
-  using K = Tile<T, kCols, MB, BM, BN, WM, WN, NB, DA, DB>;
+template <typename T, int MB, class S, bool DA, bool DB>
+__global__ __launch_bounds__(S::kThreads, S::kWorkgroups) void weight_product_kernel(WeightProduct g) {
+  using K = Tile<T, kCols, MB, S, DA, DB>;
+  constexpr int BM = S::BM, BN = S::BN, WM = S::WM, WN = S::WN;
   __shared__ __align__(16) char smem[K::kLds];
   const int per = g.tiles_m * g.tiles_n;
   const int id = by_xcd(blockIdx.x, g.chunk), unit = id / per;
-  if (unit >= g.units) return;
   int tm, tn;
   banded(id - unit * per, g.tiles_m, g.tiles_n, &tm, &tn);
-  int e, i = 0;
+  // every expert has a first part, if an empty one
+  Span t;
   if (g.part > g.rows) {
-    e = nth_longest(g.offsets, g.experts, g.rows, unit);
+    if (unit >= g.experts) return;
+    t.expert = nth_longest(g.offsets, g.experts, g.rows, unit);
+    t.index = 0;
+    t.row0 = min(max(g.offsets[t.expert], 0), g.rows);
+    t.end = min(max(g.offsets[t.expert + 1], 0), g.rows);
   } else {
-    // as in find_tile; every expert has a first part, if an empty one
-    if (!find_slot(g.offsets, g.experts, g.rows, g.part, unit, &e, &i)) return;
+    if (unit >= count_groups(g.offsets, g.experts, g.rows, g.part, 1)) return;
+    t = find_group(g.offsets, g.experts, g.rows, g.part, 1, unit);
   }
-  const int first = min(max(g.offsets[e], 0), g.rows), end = min(max(g.offsets[e + 1], 0), g.rows);
-  const int len = max(end - first, 0);
-  if (i > 0 && int64_t(i) * g.part >= len) return;
-  const int row0 = __builtin_amdgcn_readfirstlane(first + i * g.part);
-  const int depth = __builtin_amdgcn_readfirstlane(min(g.part, len - i * g.part));
-  const bool whole = len <= g.part;
+  const int e = t.expert, i = t.index;
+  const int row0 = __builtin_amdgcn_readfirstlane(t.row0);
+  const int depth = __builtin_amdgcn_readfirstlane(max(min(t.end - t.row0, g.part), 0));
+  const int first = row0 - i * g.part;
+  const bool whole = t.end - first <= g.part;
   const int m0 = tm * BM, n0 = tn * BN;
   Source a, b;
   typename K::CodeSource c;
@@ -673,7 +738,7 @@ __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64, BM * BN <= 128 * 128 ? 
     b.wide = g.k >= 8;
   }
   f32x16 acc[K::kMI][K::kNI];
-  K::template product<4>(a, b, c, depth, smem, acc);
+  K::template product<512 / S::KS>(a, b, c, depth, smem, acc);
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wm = (wave / K::kWavesN) * WM, wn = (wave % K::kWavesN) * WN;
@@ -746,14 +811,15 @@ unsigned grid_of(int64_t tiles, int64_t chunk) { return unsigned((tiles + 8 * ch
 // ---------------------------------------------------------------------------
 // Choice of tiles
 // ---------------------------------------------------------------------------
-// Microseconds of a stage of 64 contraction values where every CU has its
-// `at_once` tiles, and of a tile besides (start and output).
+// Microseconds of a stage of 64 contraction values where a CU has one tile and
+// where it has `at_once`, and of a tile besides (start and output); measured at
+// contractions of 1000 to 8192 with one to 4096 tiles.
 struct TileCost {
   int bm, bn, at_once;
-  double stage, rest;
+  double alone, full, rest;
 };
-constexpr TileCost kRowTiles[3] = {{256, 256, 1, 1.05, 6.0}, {128, 128, 2, 0.62, 4.0}, {64, 64, 2, 0.30, 3.0}};
-constexpr TileCost kWeightTiles[3] = {{256, 128, 1, 0.62, 6.0}, {128, 128, 2, 0.75, 5.0}, {64, 64, 2, 0.35, 3.0}};
+constexpr TileCost kRowTiles[3] = {{256, 256, 1, 1.3, 1.6, 5.0}, {128, 128, 2, 0.65, 0.93, 4.0}, {64, 64, 2, 0.25, 0.40, 2.5}};
+constexpr TileCost kWeightTiles[3] = {{256, 128, 1, 0.7, 1.0, 6.0}, {128, 128, 2, 0.6, 1.05, 5.0}, {64, 64, 2, 0.24, 0.45, 2.5}};
 
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
@@ -764,8 +830,12 @@ int row_tile(int64_t rows, int64_t experts, int64_t width, int64_t depth, int cu
   double least = 0.0;
   for (int i = 0; i < 3; ++i) {
     const TileCost& c = kRowTiles[i];
-    const int64_t tiles = (rows / c.bm + std::min<int64_t>(experts, rows) / 2 + 1) * ceil_div(width, c.bn);
-    const double t = double(ceil_div(tiles, int64_t(cus) * c.at_once)) * (c.stage * double(ceil_div(depth, 64)) + c.rest);
+    const int64_t e = std::min(experts, rows);
+    const int64_t tiles = (e == 1 ? ceil_div(rows, c.bm) : rows / c.bm + (e + 1) / 2) * ceil_div(width, c.bn);
+    const int64_t places = int64_t(cus) * c.at_once, left = tiles % places;
+    const double stages = double(ceil_div(depth, 64));
+    double t = double(tiles / places) * (c.full * stages + c.rest);
+    if (left > 0) t += (left <= cus && i > 0 ? c.alone : left * 4 <= cus ? c.alone : c.full) * stages + c.rest;
     if (i == 0 || t < least) {
       best = i;
       least = t;
@@ -775,8 +845,9 @@ int row_tile(int64_t rows, int64_t experts, int64_t width, int64_t depth, int cu
 }
 
 // Tile of a weight gradient and the rows of a part (WeightProduct). Whole
-// experts cost the longest one's rows, taken as three times the mean; parts as long as an even
-// share of the rows, and 12 bytes of traffic for each partial value at 4 TB/s.
+// experts take as long as the longest one, taken as three times the mean, or as
+// all of them spread evenly; parts as long as an even share and a third, with 12
+// bytes of traffic for each partial value at 4 TB/s and a second launch.
 struct WeightPlan {
   int tile;
   int64_t part;
@@ -786,11 +857,11 @@ WeightPlan weight_plan(int64_t rows, int64_t experts, int64_t n, int64_t k, int 
   double least = -1.0;
   for (int i = 0; i < 3; ++i) {
     const TileCost& c = kWeightTiles[i];
-    const int64_t per = ceil_div(n, c.bm) * ceil_div(k, c.bn);
-    const double share = double(rows) * double(per) / double(int64_t(cus) * c.at_once);   // rows of a tile's place
+    const int64_t per = ceil_div(n, c.bm) * ceil_div(k, c.bn), tiles = experts * per, places = int64_t(cus) * c.at_once;
+    const double share = double(rows) * double(per) / double(places);      // rows of each place
     const double longest = experts == 1 ? double(rows) : std::min(double(rows), 3.0 * double(rows) / double(experts));
-    const double rounds = std::max(1.0, double(experts * per) / double(int64_t(cus) * c.at_once));
-    const double whole = std::max(share, longest) / 64.0 * c.stage + rounds * c.rest;
+    const double rest = std::max(1.0, double(tiles) / double(places)) * c.rest;
+    const double whole = std::max(share * c.full, longest * (tiles <= cus ? c.alone : c.full)) / 64.0 + rest;
     if (least < 0.0 || whole < least) {
       least = whole;
       best = WeightPlan{i, rows + 1};
@@ -798,7 +869,7 @@ WeightPlan weight_plan(int64_t rows, int64_t experts, int64_t n, int64_t k, int 
     const int64_t part = std::max<int64_t>(256, ceil_div(int64_t(share) + 1, 64) * 64);
     if (double(part) < longest / 1.25) {
       const double parts = double(rows) / double(part) + (experts == 1 ? 1.0 : 0.0);
-      const double split = 1.3 * double(part) / 64.0 * c.stage + rounds * c.rest + parts * double(n) * double(k) * 12.0 / 4e6 + 6.0;
+      const double split = 1.33 * double(part) / 64.0 * c.full + rest + parts * double(n) * double(k) * 12.0 / 4e6 + 6.0;
       if (split < least) {
         least = split;
         best = WeightPlan{i, part};
@@ -811,30 +882,28 @@ WeightPlan weight_plan(int64_t rows, int64_t experts, int64_t n, int64_t k, int 
 // Slots of partial sums that parts of that many rows can need.
 int64_t partial_slots(int64_t rows, int64_t part) { return part > rows ? 0 : 2 * rows / part + 1; }
 
-template <typename T, int MB, int BM, int BN, int WM, int WN, int NB>
+// S: shape where both operands are copied straight to LDS, R: otherwise.
+template <typename T, int MB, class S, class R>
 void run_rows(RowProduct g, bool da, bool db, hipStream_t stream) {
-  g.slots = g.rows / BM + g.experts;
-  g.tiles_n = (g.width + BN - 1) / BN;
-  // one run an XCD: tiles cost the same
-  const int64_t tiles = int64_t(g.slots) * g.tiles_n;
-  g.chunk = int((tiles + 7) / 8);
-  const dim3 grid(grid_of(tiles, g.chunk));
-  constexpr int kThreads = (BM / WM) * (BN / WN) * 64;
+  g.tiles_n = (g.width + S::BN - 1) / S::BN;
+  // the most tiles that any split of the rows into experts makes
+  const int64_t tiles = (int64_t(g.rows) / S::BM + std::min(g.experts, g.rows)) * g.tiles_n;
+  const dim3 grid(unsigned((tiles + 7) / 8 * 8));
   if (da && db) {
-    row_product_kernel<T, MB, BM, BN, WM, WN, NB, true, true><<<grid, kThreads, 0, stream>>>(g);
+    row_product_kernel<T, MB, S, true, true><<<grid, S::kThreads, 0, stream>>>(g);
     return;
   }
   if constexpr (MB == kCols) {       // (rows of Y = X W^T's operands are alike)
     if (db) {
-      row_product_kernel<T, MB, BM, BN, WM, WN, NB, false, true><<<grid, kThreads, 0, stream>>>(g);
+      row_product_kernel<T, MB, R, false, true><<<grid, R::kThreads, 0, stream>>>(g);
       return;
     }
     if (da) {
-      row_product_kernel<T, MB, BM, BN, WM, WN, NB, true, false><<<grid, kThreads, 0, stream>>>(g);
+      row_product_kernel<T, MB, R, true, false><<<grid, R::kThreads, 0, stream>>>(g);
       return;
     }
   }
-  row_product_kernel<T, MB, BM, BN, WM, WN, NB, false, false><<<grid, kThreads, 0, stream>>>(g);
+  row_product_kernel<T, MB, R, false, false><<<grid, R::kThreads, 0, stream>>>(g);
 }
 
 template <typename T, int MB>
@@ -858,29 +927,28 @@ void row_product(const GroupArgs& x, int width, int depth, hipStream_t stream) {
   const bool da = aligned16(x.a) && x.lda % 8 == 0 && depth % 8 == 0;
   const bool db = aligned16(x.b) && x.ldb % 8 == 0 && x.b_stride % 8 == 0 && (MB == kCols || depth % 8 == 0);
   switch (row_tile(x.rows, x.experts, width, depth, x.cus)) {
-    case 0: run_rows<T, MB, 256, 256, 128, 128, 2>(g, da, db, stream); break;
-    case 1: run_rows<T, MB, 128, 128, 64, 64, 2>(g, da, db, stream); break;
-    default: run_rows<T, MB, 64, 64, 32, 32, 4>(g, da, db, stream); break;
+    case 0: run_rows<T, MB, Shape<256, 256, 128, 64, 64, 2, 2>, Shape<256, 256, 128, 64, 64, 2, 1>>(g, da, db, stream); break;
+    case 1: run_rows<T, MB, Shape<128, 128, 64, 64, 64, 2, 2>, Shape<128, 128, 64, 64, 64, 2, 1>>(g, da, db, stream); break;
+    default: run_rows<T, MB, Shape<64, 64, 32, 32, 64, 4, 4>, Shape<64, 64, 32, 32, 64, 4, 4>>(g, da, db, stream); break;
   }
 }
 
-template <typename T, int MB, int BM, int BN, int WM, int WN, int NB>
+template <typename T, int MB, class S, class R>
 void run_weight(WeightProduct g, bool da, bool db, hipStream_t stream) {
-  g.tiles_m = (g.n + BM - 1) / BM;
-  g.tiles_n = (g.k + BN - 1) / BN;
+  g.tiles_m = (g.n + S::BM - 1) / S::BM;
+  g.tiles_n = (g.k + S::BN - 1) / S::BN;
   // an expert's tiles over all XCDs: those of one expert cost the same
   const int64_t per = int64_t(g.tiles_m) * g.tiles_n;
   g.chunk = int((per + 7) / 8);
-  const dim3 grid(grid_of(per * g.units, g.chunk));
-  constexpr int kThreads = (BM / WM) * (BN / WN) * 64;
+  const dim3 grid(grid_of(per * (g.rows / g.part + g.experts), g.chunk));
   if constexpr (MB == kCodes) {
-    if (da) weight_product_kernel<T, MB, BM, BN, WM, WN, NB, true, false><<<grid, kThreads, 0, stream>>>(g);
-    else weight_product_kernel<T, MB, BM, BN, WM, WN, NB, false, false><<<grid, kThreads, 0, stream>>>(g);
+    if (da) weight_product_kernel<T, MB, R, true, false><<<grid, R::kThreads, 0, stream>>>(g);
+    else weight_product_kernel<T, MB, R, false, false><<<grid, R::kThreads, 0, stream>>>(g);
   } else {
-    if (da && db) weight_product_kernel<T, MB, BM, BN, WM, WN, NB, true, true><<<grid, kThreads, 0, stream>>>(g);
-    else if (db) weight_product_kernel<T, MB, BM, BN, WM, WN, NB, false, true><<<grid, kThreads, 0, stream>>>(g);
-    else if (da) weight_product_kernel<T, MB, BM, BN, WM, WN, NB, true, false><<<grid, kThreads, 0, stream>>>(g);
-    else weight_product_kernel<T, MB, BM, BN, WM, WN, NB, false, false><<<grid, kThreads, 0, stream>>>(g);
+    if (da && db) weight_product_kernel<T, MB, S, true, true><<<grid, S::kThreads, 0, stream>>>(g);
+    else if (db) weight_product_kernel<T, MB, R, false, true><<<grid, R::kThreads, 0, stream>>>(g);
+    else if (da) weight_product_kernel<T, MB, R, true, false><<<grid, R::kThreads, 0, stream>>>(g);
+    else weight_product_kernel<T, MB, R, false, false><<<grid, R::kThreads, 0, stream>>>(g);
   }
 }
 
@@ -904,12 +972,11 @@ void weight_product(const GroupArgs& x, hipStream_t stream) {
   g.k = x.k;
   g.accumulate = x.accumulate;
   g.part = int(plan.part);
-  g.units = int(x.rows / plan.part) + x.experts;
   const bool da = aligned16(x.a) && x.lda % 8 == 0, db = MB != kCodes && aligned16(x.b) && x.ldb % 8 == 0;
   switch (plan.tile) {
-    case 0: run_weight<T, MB, 256, 128, 128, 64, 3>(g, da, db, stream); break;
-    case 1: run_weight<T, MB, 128, 128, 64, 64, 2>(g, da, db, stream); break;
-    default: run_weight<T, MB, 64, 64, 32, 32, 4>(g, da, db, stream); break;
+    case 0: run_weight<T, MB, Shape<256, 128, 64, 64, 64, 3, 2>, Shape<256, 128, 64, 64, 64, 3, 1>>(g, da, db, stream); break;
+    case 1: run_weight<T, MB, Shape<128, 128, 64, 64, 64, 2, 1>, Shape<128, 128, 64, 64, 64, 2, 1>>(g, da, db, stream); break;
+    default: run_weight<T, MB, Shape<64, 64, 32, 32, 64, 4, 4>, Shape<64, 64, 32, 32, 64, 4, 4>>(g, da, db, stream); break;
   }
   if (plan.part <= x.rows) {
     const int64_t blocks = ceil_div(x.k, 1024);
