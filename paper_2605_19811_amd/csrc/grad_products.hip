@@ -195,17 +195,18 @@ struct Source {
 };
 
 // KS: contraction values of a stage; NB: stages in LDS; SUB: groups of 16 values of
-// a step (below); DA, DB: the operand goes straight to LDS, else through registers.
-template <int BM_, int BN_, int WM_, int WN_, int KS_, int NB_, int SUB_>
+// a step (below); PRE: stages that are loaded ahead into registers, for operands that
+// go through them. DA, DB: the operand goes straight to LDS, else through registers.
+template <int BM_, int BN_, int WM_, int WN_, int KS_, int NB_, int SUB_, int PRE_ = 1>
 struct Shape {
-  static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, KS = KS_, NB = NB_, SUB = SUB_;
+  static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, KS = KS_, NB = NB_, SUB = SUB_, PRE = PRE_;
   static constexpr int kWavesN = BN / WN, kWaves = (BM / WM) * kWavesN, kThreads = kWaves * 64;
   static constexpr int kWorkgroups = BM * BN <= 128 * 128 ? 2 : 1;      // on a CU at least
 };
 
 template <typename T, int MA, int MB, class S, bool DA, bool DB>
 struct Tile {
-  static constexpr int BM = S::BM, BN = S::BN, WM = S::WM, WN = S::WN, KS = S::KS, NB = S::NB, SUB = S::SUB;
+  static constexpr int BM = S::BM, BN = S::BN, WM = S::WM, WN = S::WN, KS = S::KS, NB = S::NB, SUB = S::SUB, PRE = S::PRE;
   static constexpr int kWavesN = S::kWavesN, kWaves = S::kWaves, kThreads = S::kThreads;
   static constexpr int kMI = WM / 32, kNI = WN / 32;
   static constexpr int kStageA = BM * KS * 2, kStageBytes = (BM + BN) * KS * 2;
@@ -399,29 +400,30 @@ struct Tile {
     constexpr int kPiecesB = MB == kCodes ? kPieces : 0;
     Copier<MA, BM> ca(a, wave, lane);
     Copier<kModeB, BN> cb(b, wave, lane);
-    Regs<MA, DA ? 0 : BM> ra;
-    Regs<kModeB, (DB || MB == kCodes) ? 0 : BN> rb;
-    CodeRegs rc;
-    // stages that go through registers: loaded one stage ahead of the write to LDS
-    auto load = [&](int kt) {
-      if constexpr (!DA) fetch<MA, BM>(a, kt * KS, tid, ra);
-      if constexpr (!DB && MB != kCodes) fetch<kModeB, BN>(b, kt * KS, tid, rb);
+    Regs<MA, DA ? 0 : BM> ra[PRE];
+    Regs<kModeB, (DB || MB == kCodes) ? 0 : BN> rb[PRE];
+    CodeRegs rc[PRE];
+    // stages that go through registers: loaded PRE stages ahead of the write to
+    // LDS, into register set kt % PRE
+    auto load = [&](int kt, int set) {
+      if constexpr (!DA) fetch<MA, BM>(a, kt * KS, tid, ra[set]);
+      if constexpr (!DB && MB != kCodes) fetch<kModeB, BN>(b, kt * KS, tid, rb[set]);
     };
-    auto load_codes = [&](int kt) {
-      if constexpr (MB == kCodes) fetch(c, kt * KS, tid, rc);
+    auto load_codes = [&](int kt, int set) {
+      if constexpr (MB == kCodes) fetch(c, kt * KS, tid, rc[set]);
     };
     constexpr int kWritesA = DA ? 0 : Regs<MA, BM>::kInst, kWritesB = (DB || MB == kCodes) ? 0 : Regs<kModeB, BN>::kInst;
     constexpr int kWrites = kWritesA + kWritesB;
-    auto write = [&](int kt, int q, char* buf) {
+    auto write = [&](int kt, int set, int q, char* buf) {
       if constexpr (!DA) {
         if (q < kWritesA) {
-          put<MA, BM>(a, kt * KS, ra, q, buf, tid);
+          put<MA, BM>(a, kt * KS, ra[set], q, buf, tid);
           return;
         }
       }
-      if constexpr (!DB && MB != kCodes) put<kModeB, BN>(b, kt * KS, rb, q - kWritesA, buf + kStageA, tid);
+      if constexpr (!DB && MB != kCodes) put<kModeB, BN>(b, kt * KS, rb[set], q - kWritesA, buf + kStageA, tid);
     };
-    auto widen = [&](int piece, char* buf) { put(rc, piece, buf + kStageA, tid); };
+    auto widen = [&](int set, int piece, char* buf) { put(rc[set], piece, buf + kStageA, tid); };
     auto start = [&](int kt) {
       if constexpr (DA) ca.start(kt * KS);
       if constexpr (DB) cb.start(kt * KS);
@@ -443,6 +445,8 @@ struct Tile {
     };
     zero(out);
     if (nk == 0) return;
+    // the slots' pattern repeats after kTurns stages
+    constexpr int kTurns = PRE > 1 ? (PRE % 2 == 0 ? PRE : 2 * PRE) : KS / 16 / SUB % 2 == 0 ? 1 : 2;
     constexpr int kSteps = KS / 16 / SUB, kFrags = SUB * (kMI + kNI), kMfmas = SUB * kMI * kNI;
     // A stage's copies start in the last step of stage kt - NB, and, with more than
     // two buffers, which leave them time to land, go on through that of the next
@@ -458,20 +462,26 @@ struct Tile {
       for (int q = 0; q < (kt + 1 < NB ? kCopies : kFirst); ++q) copy(q, kt * kStageBytes);
     }
     if constexpr (kWrites + kPiecesB > 0) {
+      // (stage kt + PRE is asked for before stage kt is written)
+      static_assert(NB % PRE == 0, "stage NB's set is the first again");
+#pragma unroll
+      for (int kt = 0; kt < PRE; ++kt) {
+        if (kt < nk) load(kt, kt);
+        load_codes(kt, kt);
+      }
+#pragma unroll
       for (int kt = 0; kt < NB; ++kt) {
         char* to = smem + kt * kStageBytes;
         if (kt < nk) {
-          load(kt);
 #pragma unroll
-          for (int q = 0; q < kWrites; ++q) write(kt, q, to);
+          for (int q = 0; q < kWrites; ++q) write(kt, kt % PRE, q, to);
         }
-        load_codes(kt);
 #pragma unroll
-        for (int h = 0; h < kPiecesB; ++h) widen(h, to);
+        for (int h = 0; h < kPiecesB; ++h) widen(kt % PRE, h, to);
+        if (kt + PRE < nk) load(kt + PRE, kt % PRE);
+        load_codes(kt + PRE, kt % PRE);
       }
     }
-    if (NB < nk) load(NB);
-    load_codes(NB);
     if constexpr (kCopies > 0) wait_vmcnt<(NB - 2) * kCopies + kFirst>();
     lds_barrier();
     s16x8 fa[2][SUB * kMI], fb[2][SUB * kNI];
@@ -487,7 +497,7 @@ struct Tile {
     // One step (fragments in slot `cur`): its MFMAs, each followed by its share of the
     // next step's reads (step st1 of the stage at buf1), of copies q0 .. q1 to
     // `fill` and, in the last step, of the writes to it.
-    auto step = [&](int cur, int buf1, int st1, int fill, int q0, int q1, bool last, int kt) {
+    auto step = [&](int cur, int buf1, int st1, int fill, int q0, int q1, bool last, int kt, int set) {
 #pragma unroll
       for (int m = 0; m < kMfmas; ++m) {
         const int u = m / (kMI * kNI), i = m / kNI % kMI, j = m % kNI;
@@ -502,9 +512,9 @@ struct Tile {
         if (regs) {
           constexpr int kD = kParts > 0 ? kParts : 1;
 #pragma unroll
-          for (int h = m * kPiecesB / kD; h < (m + 1) * kPiecesB / kD; ++h) widen(h, smem + fill);
+          for (int h = m * kPiecesB / kD; h < (m + 1) * kPiecesB / kD; ++h) widen(set, h, smem + fill);
 #pragma unroll
-          for (int q = m * kWrites / kD; q < (m + 1) * kWrites / kD; ++q) write(kt, q, smem + fill);
+          for (int q = m * kWrites / kD; q < (m + 1) * kWrites / kD; ++q) write(kt, set, q, smem + fill);
         }
         if (!regs || kMfmas == 1) {
           const int at = last && kMfmas > 1 ? kParts : 0, n = q1 - q0;
@@ -515,12 +525,13 @@ struct Tile {
       }
     };
     int buf = 0, filling = (NB - 1) * kStageBytes;
-    auto stage = [&](int kt, int par) {
+    auto stage = [&](int kt, int turn) {           // turn: kt modulo kTurns
+      const int par = turn * kSteps, set = turn % PRE;
       const int next = buf == (NB - 1) * kStageBytes ? 0 : buf + kStageBytes;
 #pragma unroll
       for (int st = 0; st + 1 < kSteps; ++st) {
         constexpr int kLeft = kCopies - kFirst, kOver = kSteps > 1 ? kSteps - 1 : 1;
-        step((par + st) & 1, buf, st + 1, filling, kFirst + st * kLeft / kOver, kFirst + (st + 1) * kLeft / kOver, false, 0);
+        step((par + st) & 1, buf, st + 1, filling, kFirst + st * kLeft / kOver, kFirst + (st + 1) * kLeft / kOver, false, 0, 0);
       }
       // stage kt + 1 has landed: at least that many copies of later ones
       // were started after its own
@@ -528,38 +539,28 @@ struct Tile {
       lds_barrier();
       start(kt + NB);
       __builtin_amdgcn_sched_barrier(0);
-      step((par + kSteps - 1) & 1, next, 0, buf, 0, kFirst, true, kt + NB);
+      step((par + kSteps - 1) & 1, next, 0, buf, 0, kFirst, true, kt + NB, set);
       // (the registers are free now)
-      if (kt + NB + 1 < nk) load(kt + NB + 1);
-      load_codes(kt + NB + 1);
+      if (kt + NB + PRE < nk) load(kt + NB + PRE, set);
+      load_codes(kt + NB + PRE, set);
       __builtin_amdgcn_sched_barrier(0);
       filling = buf;
       buf = next;
     };
-    // stages in [k0, k1), two at a time where a stage has an odd number of steps,
-    // so that the fragments' slots are known to the compiler
+    // Stages in [k0, k1), kTurns at a time, so that the compiler knows the slots of
+    // fragments and registers; k0 is a multiple of kTurns.
     auto stages = [&](int k0, int k1) {
-      if constexpr (kSteps % 2 == 0) {
+      int kt = k0;
 #pragma unroll 1
-        for (int kt = k0; kt < k1; ++kt) stage(kt, 0);
-      } else {
-        // (an odd one out is a whole pair's first: the slots then start over, so its
-        // fragments move once)
-        int kt = k0;
-#pragma unroll 1
-        for (; kt + 2 <= k1; kt += 2) {
-          stage(kt, 0);
-          stage(kt + 1, 1);
-        }
-        if (kt < k1) {
-          stage(kt, 0);
+      for (; kt + kTurns <= k1; kt += kTurns) {
 #pragma unroll
-          for (int f = 0; f < SUB * kMI; ++f) fa[0][f] = fa[1][f];
-#pragma unroll
-          for (int f = 0; f < SUB * kNI; ++f) fb[0][f] = fb[1][f];
-        }
+        for (int t = 0; t < kTurns; ++t) stage(kt + t, t);
       }
+#pragma unroll
+      for (int t = 0; t + 1 < kTurns; ++t)
+        if (kt + t < k1) stage(kt + t, t);
     };
+    static_assert(FOLD % kTurns == 0, "whole turns");
     if constexpr (FOLD > 0) {
       for (int k0 = 0; k0 < nk; k0 += FOLD) {
         zero(acc);
@@ -745,29 +746,52 @@ __global__ __launch_bounds__(S::kThreads, S::kWorkgroups) void weight_product_ke
   float* out = whole ? g.out + e * g.o_stride : g.partial + int64_t(partial_slot(first, g.part) + i) * g.n * g.k;
   const int64_t ldo = whole ? g.ldo : g.k;
   const bool add = whole && g.accumulate;
-  // 32 lanes write 128 bytes of a row
+  // Through LDS, 32 rows of a wave at a time, so that a lane writes 16 bytes of a row
+  constexpr int kLd = WN + 4;
+  static_assert(K::kWaves * 32 * kLd * 4 <= K::kLds, "staging fits");
+  lds_barrier();
+  float* st = reinterpret_cast<float*>(smem) + wave * 32 * kLd;
 #pragma unroll
-  for (int i = 0; i < K::kMI; ++i)
+  for (int q = 0; q < K::kMI; ++q) {
 #pragma unroll
-    for (int j = 0; j < K::kNI; ++j) {
-      const int col = n0 + wn + 32 * j + (lane & 31);
+    for (int j = 0; j < K::kNI; ++j)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        const int row = m0 + wm + 32 * i + 8 * (r >> 2) + 4 * (lane >> 5) + (r & 3);
-        if (row < g.n && col < g.k) {
-          float* p = out + int64_t(row) * ldo + col;
-          *p = add ? *p + acc[i][j][r] : acc[i][j][r];
+      for (int r = 0; r < 16; ++r) st[(8 * (r >> 2) + 4 * (lane >> 5) + (r & 3)) * kLd + 32 * j + (lane & 31)] = acc[q][j][r];
+    // (a wave's own region: its LDS accesses are in order)
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    constexpr int kPer = WN / 4;
+#pragma unroll 8
+    for (int s = 0; s < 32 * kPer / 64; ++s) {
+      const int r = (s * 64 + lane) / kPer, c = (lane % kPer) * 4;
+      const int row = m0 + wm + 32 * q + r, col = n0 + wn + c;
+      if (row >= g.n || col >= g.k) continue;
+      float v[4];
+      __builtin_memcpy(v, st + r * kLd + c, 16);
+      float* p = out + int64_t(row) * ldo + col;
+      if (col + 4 <= g.k) {
+        if (add) {
+          float t[4];
+          __builtin_memcpy(t, p, 16);
+#pragma unroll
+          for (int x = 0; x < 4; ++x) v[x] += t[x];
         }
+        __builtin_memcpy(p, v, 16);
+      } else {
+        for (int x = 0; x < 4; ++x)
+          if (col + x < g.k) p[x] = add ? p[x] + v[x] : v[x];
       }
     }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+  }
 }
 
-// dW_e = (dW_e +) the sum of the parts of an expert that has several, in their
-// order: four columns a thread, `blocks` workgroups a row of dW. Workgroups of
-// the nth such expert, of at most rows / part.
+// dW_e = (dW_e +) the sum of the parts of an expert that has several: 256
+// values of dW a workgroup, four a lane, every fourth part a wave; the waves' sums
+// meet in LDS. `blocks` workgroups for the nth such expert.
 __global__ __launch_bounds__(256) void weight_reduce_kernel(WeightProduct g, int blocks) {
-  const int line = blockIdx.x / blocks, nth = line / g.n, row = line - nth * g.n;
-  const int lane = threadIdx.x & 63;
+  __shared__ float sums[3][64][4];
+  const int nth = blockIdx.x / blocks;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   int e = -1, seen = 0;
   for (int base = 0; base < g.experts; base += 64) {
     const int i = min(base + lane, g.experts - 1);
@@ -784,13 +808,12 @@ __global__ __launch_bounds__(256) void weight_reduce_kernel(WeightProduct g, int
   if (e < 0) return;
   const int first = min(max(g.offsets[e], 0), g.rows), len = min(max(g.offsets[e + 1], 0), g.rows) - first;
   const int parts = (len + g.part - 1) / g.part;
-  const int col = ((blockIdx.x - line * blocks) * 256 + threadIdx.x) * 4, m = min(4, g.k - col);
-  if (m <= 0) return;
-  const int64_t one = int64_t(g.n) * g.k;
-  const float* p = g.partial + partial_slot(first, g.part) * one + int64_t(row) * g.k + col;
-  float* o = g.out + e * g.o_stride + row * g.ldo + col;
+  const int64_t one = int64_t(g.n) * g.k, at = (int64_t(blockIdx.x - nth * blocks) * 64 + lane) * 4;
+  const int m = int(min(one - at, int64_t(4)));
+  const float* p = g.partial + partial_slot(first, g.part) * one + at;
   float v[4] = {0.f, 0.f, 0.f, 0.f};
-  for (int s = 0; s < parts; ++s) {
+#pragma unroll 4
+  for (int s = wave; s < parts; s += 4) {
     if (m == 4) {
       float t[4];
       __builtin_memcpy(t, p + s * one, 16);
@@ -800,7 +823,22 @@ __global__ __launch_bounds__(256) void weight_reduce_kernel(WeightProduct g, int
       for (int j = 0; j < m; ++j) v[j] += p[s * one + j];
     }
   }
-  for (int j = 0; j < m; ++j) o[j] = g.accumulate ? o[j] + v[j] : v[j];
+  if (wave > 0) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) sums[wave - 1][lane][j] = v[j];
+  }
+  __syncthreads();
+  if (wave > 0) return;
+#pragma unroll
+  for (int w = 0; w < 3; ++w)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v[j] += sums[w][lane][j];
+  float* o = g.out + e * g.o_stride;
+  for (int j = 0; j < m; ++j) {
+    const uint32_t row = uint32_t(uint64_t(at + j) / uint32_t(g.k)), col = uint32_t(at + j - int64_t(row) * g.k);
+    float* q = o + row * g.ldo + col;
+    *q = g.accumulate ? *q + v[j] : v[j];
+  }
 }
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
@@ -928,8 +966,8 @@ void row_product(const GroupArgs& x, int width, int depth, hipStream_t stream) {
   const bool db = aligned16(x.b) && x.ldb % 8 == 0 && x.b_stride % 8 == 0 && (MB == kCols || depth % 8 == 0);
   switch (row_tile(x.rows, x.experts, width, depth, x.cus)) {
     case 0: run_rows<T, MB, Shape<256, 256, 128, 64, 64, 2, 2>, Shape<256, 256, 128, 64, 64, 2, 1>>(g, da, db, stream); break;
-    case 1: run_rows<T, MB, Shape<128, 128, 64, 64, 64, 2, 2>, Shape<128, 128, 64, 64, 64, 2, 1>>(g, da, db, stream); break;
-    default: run_rows<T, MB, Shape<64, 64, 32, 32, 64, 4, 4>, Shape<64, 64, 32, 32, 64, 4, 4>>(g, da, db, stream); break;
+    case 1: run_rows<T, MB, Shape<128, 128, 64, 64, 64, 2, 2>, Shape<128, 128, 64, 64, 64, 2, 1, 2>>(g, da, db, stream); break;
+    default: run_rows<T, MB, Shape<64, 64, 32, 32, 64, 4, 4>, Shape<64, 64, 32, 32, 64, 4, 4, 4>>(g, da, db, stream); break;
   }
 }
 
@@ -976,11 +1014,12 @@ void weight_product(const GroupArgs& x, hipStream_t stream) {
   switch (plan.tile) {
     case 0: run_weight<T, MB, Shape<256, 128, 64, 64, 64, 3, 2>, Shape<256, 128, 64, 64, 64, 3, 1>>(g, da, db, stream); break;
     case 1: run_weight<T, MB, Shape<128, 128, 64, 64, 64, 2, 1>, Shape<128, 128, 64, 64, 64, 2, 1>>(g, da, db, stream); break;
-    default: run_weight<T, MB, Shape<64, 64, 32, 32, 64, 4, 4>, Shape<64, 64, 32, 32, 64, 4, 4>>(g, da, db, stream); break;
+    default: run_weight<T, MB, Shape<64, 64, 32, 32, 64, 4, 4>, Shape<64, 64, 32, 32, 64, 4, 4, 4>>(g, da, db, stream); break;
   }
   if (plan.part <= x.rows) {
-    const int64_t blocks = ceil_div(x.k, 1024);
-    weight_reduce_kernel<<<dim3(unsigned(blocks * x.n * (x.rows / plan.part))), 256, 0, stream>>>(g, int(blocks));
+    const int64_t blocks = ceil_div(int64_t(x.n) * x.k, 256);
+    const int64_t several = std::min<int64_t>(x.experts, x.rows / plan.part);    // experts of more rows than a part
+    weight_reduce_kernel<<<dim3(unsigned(blocks * several)), 256, 0, stream>>>(g, int(blocks));
   }
 }
 
