@@ -6,6 +6,8 @@
 // 128 columns that share a scale, so a checkpoint's maximum is four lane
 // rotations away, without LDS, and every kernel that has a tensor in registers
 // can store its checkpoint on the way.
+#include <type_traits>
+
 #include "grad_device.h"
 
 namespace lm {
@@ -60,28 +62,6 @@ __device__ __forceinline__ void put8(const CkptView& k, int64_t row, int64_t c, 
   if ((c & (kCkptBlock - 1)) == 0 && c < cols) k.scales[row * k.ld_scales + c / kCkptBlock] = uint8_t(scale);
 }
 
-// Values of columns c .. c + 7 of a checkpoint's row, of which n exist; c need
-// not be a multiple of 8 (the second half of a gated activation's input).
-__device__ __forceinline__ void get8(const CkptView& k, int64_t row, int64_t c, int64_t n, float v[8]) {
-  const uint8_t* p = k.codes + row * k.ld_codes + c;
-  u32x2 w = {0u, 0u};
-  if (n >= 8) {
-    __builtin_memcpy(&w, p, 8);
-  } else {
-#pragma unroll
-    for (int j = 0; j < 8; ++j)
-      if (j < n) w[j >> 2] |= uint32_t(p[j]) << (8 * (j & 3));
-  }
-  const uint8_t* s = k.scales + row * k.ld_scales;
-  const int64_t last = c + (n < 8 ? n : 8) - 1;
-  const int64_t b0 = c / kCkptBlock, b1 = (last < c ? c : last) / kCkptBlock;
-  decode8(w, 1.0f, v);
-  const float s0 = n > 0 ? scale_of(s[b0]) : 0.0f, s1 = n > 0 ? scale_of(s[b1]) : 0.0f;
-  const int64_t edge = (b0 + 1) * kCkptBlock - c;
-#pragma unroll
-  for (int j = 0; j < 8; ++j) v[j] *= j < edge ? s0 : s1;
-}
-
 // ---------------------------------------------------------------------------
 // Kernels over blocks of 128 columns: checkpoint, restore, activation
 // ---------------------------------------------------------------------------
@@ -105,22 +85,101 @@ BlockWalk walk_of(int64_t rows, int64_t cols) {
   return w;
 }
 
-template <class F>
-__device__ __forceinline__ void for_blocks(const BlockWalk& w, F f) {
+// load(row, column) gives what a lane needs of its eight columns, use(row, column,
+// that) does the rest: a group has the loads of two blocks in flight.
+template <class L, class U>
+__device__ __forceinline__ void for_blocks(const BlockWalk& w, L load, U use) {
+  constexpr int kGroups = kRowThreads / 16;
   const int64_t row0 = int64_t(blockIdx.x) * w.per;
   const int64_t left = w.rows - row0;
   const int total = int(left < w.per ? left : w.per) * w.blocks;
-  for (int i = threadIdx.x >> 4; i < total; i += kRowThreads / 16) {
+  auto place = [&](int i, int64_t* row, int64_t* c) {
     const int r = i / w.blocks;
-    f(row0 + r, int64_t(i - r * w.blocks) * kCkptBlock + (threadIdx.x & 15) * 8);
+    *row = row0 + r;
+    *c = int64_t(i - r * w.blocks) * kCkptBlock + (threadIdx.x & 15) * 8;
+  };
+  for (int i = threadIdx.x >> 4; i < total; i += 2 * kGroups) {
+    int64_t r0, c0, r1, c1;
+    place(i, &r0, &c0);
+    const bool two = i + kGroups < total;
+    place(two ? i + kGroups : i, &r1, &c1);
+    auto d0 = load(r0, c0);
+    auto d1 = d0;
+    if (two) d1 = load(r1, c1);
+    use(r0, c0, d0);
+    if (two) use(r1, c1, d1);
   }
 }
+
+// What is loaded of eight values, before it is converted.
+template <typename T>
+struct Raw {
+  T v[8];
+  __device__ __forceinline__ void load(const T* p, int64_t n) {
+    if (n >= 8) {
+      __builtin_memcpy(v, p, sizeof(v));
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] = j < n ? p[j] : T(0.0f);
+    }
+  }
+  __device__ __forceinline__ void get(float o[8]) const {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) o[j] = float(v[j]);
+  }
+};
+// Eight codes of a checkpoint from column c on, with the scale of their block. ANY: c
+// need not be a multiple of 8, and the codes may lie in two blocks.
+template <bool ANY = false>
+struct RawCodes {
+  u32x2 w;
+  uint32_t s0, s1;
+  int edge;            // codes of the first block
+  __device__ __forceinline__ void load(const CkptView& k, int64_t row, int64_t c, int64_t n) {
+    w = u32x2{0u, 0u};
+    s0 = s1 = 0;
+    edge = 8;
+    if (n <= 0) return;
+    const uint8_t* p = k.codes + row * k.ld_codes + c;
+    if (!ANY) {
+      // (rows of codes reach to a multiple of 16)
+      w = *reinterpret_cast<const u32x2*>(p);
+    } else if (n >= 8) {
+      __builtin_memcpy(&w, p, 8);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        if (j < n) w[j >> 2] |= uint32_t(p[j]) << (8 * (j & 3));
+    }
+    const uint8_t* s = k.scales + row * k.ld_scales;
+    const int64_t b0 = c / kCkptBlock;
+    s0 = s[b0];
+    if constexpr (ANY) {
+      s1 = s[(c + (n < 8 ? n : 8) - 1) / kCkptBlock];
+      edge = int((b0 + 1) * kCkptBlock - c);
+    }
+  }
+  __device__ __forceinline__ void get(float o[8]) const {
+    if constexpr (ANY) {
+      decode8(w, 1.0f, o);
+      const float f0 = scale_of(s0), f1 = scale_of(s1);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) o[j] *= j < edge ? f0 : f1;
+    } else {
+      decode8(w, scale_of(s0), o);
+    }
+  }
+};
 
 template <typename T>
 __global__ __launch_bounds__(kRowThreads) void checkpoint_kernel(BlockWalk w, MatView x, CkptView out) {
   for_blocks(w, [&](int64_t row, int64_t c) {
+    Raw<T> d;
+    d.load(static_cast<const T*>(x.data) + row * x.ld + c, w.cols - c);
+    return d;
+  }, [&](int64_t row, int64_t c, const Raw<T>& d) {
     float v[8];
-    load8(static_cast<const T*>(x.data) + row * x.ld + c, w.cols - c, v);
+    d.get(v);
     u32x2 codes;
     const uint32_t s = encode8(v, &codes);
     put8(out, row, c, w.cols, codes, s);
@@ -130,8 +189,12 @@ __global__ __launch_bounds__(kRowThreads) void checkpoint_kernel(BlockWalk w, Ma
 template <typename T>
 __global__ __launch_bounds__(kRowThreads) void restore_kernel(BlockWalk w, CkptView k, MatView out) {
   for_blocks(w, [&](int64_t row, int64_t c) {
+    RawCodes<> d;
+    d.load(k, row, c, w.cols - c);
+    return d;
+  }, [&](int64_t row, int64_t c, const RawCodes<>& d) {
     float v[8];
-    get8(k, row, c, w.cols - c, v);
+    d.get(v);
     store8(static_cast<T*>(out.data) + row * out.ld + c, w.cols - c, v);
   });
 }
@@ -157,12 +220,20 @@ __device__ __forceinline__ float gelu_gate(float x) {
 // blocks then have to start at multiples of 128 columns.
 template <typename T, int KIND, bool KEEP>
 __global__ __launch_bounds__(kRowThreads) void activation_kernel(BlockWalk w, MatView a, MatView h, CkptView kept) {
+  struct Data {
+    Raw<T> x, u;
+  };
   const int64_t cols = w.cols;
   for_blocks(w, [&](int64_t row, int64_t c) {
     const T* p = static_cast<const T*>(a.data) + row * a.ld + c;
+    Data d;
+    d.x.load(p, cols - c);
+    if constexpr (KIND == kSwiglu) d.u.load(p + cols, cols - c);
+    return d;
+  }, [&](int64_t row, int64_t c, const Data& d) {
     float x[8], u[8], o[8];
-    load8(p, cols - c, x);
-    if constexpr (KIND == kSwiglu) load8(p + cols, cols - c, u);
+    d.x.get(x);
+    if constexpr (KIND == kSwiglu) d.u.get(u);
 #pragma unroll
     for (int j = 0; j < 8; ++j) o[j] = KIND == kSwiglu ? x[j] * sigmoid<T>(x[j]) * u[j] : x[j] * gelu_gate<T>(x[j]);
     if constexpr (KEEP) {
@@ -181,20 +252,36 @@ __global__ __launch_bounds__(kRowThreads) void activation_kernel(BlockWalk w, Ma
 // da = dh act'(a) and, where h is given, act(a) again.
 template <typename T, int KIND, bool KEPT>
 __global__ __launch_bounds__(kRowThreads) void activation_grad_kernel(BlockWalk w, MatView dh, MatView a, CkptView kept, MatView da, MatView h) {
+  struct Whole {
+    Raw<T> d, x, u;
+  };
+  struct Kept {
+    Raw<T> d;
+    RawCodes<> x;
+    RawCodes<true> u;          // its half may start anywhere
+  };
+  using Data = std::conditional_t<KEPT, Kept, Whole>;
   const int64_t cols = w.cols;
   for_blocks(w, [&](int64_t row, int64_t c) {
     const int64_t n = cols - c;
-    if (n <= 0) return;
-    float x[8], u[8], d[8], o[8], dx[8], du[8];
-    load8(static_cast<const T*>(dh.data) + row * dh.ld + c, n, d);
+    Data d;
+    d.d.load(static_cast<const T*>(dh.data) + row * dh.ld + c, n);
     if constexpr (KEPT) {
-      get8(kept, row, c, n, x);
-      if constexpr (KIND == kSwiglu) get8(kept, row, cols + c, n, u);
+      d.x.load(kept, row, c, n);
+      if constexpr (KIND == kSwiglu) d.u.load(kept, row, cols + c, n);
     } else {
       const T* p = static_cast<const T*>(a.data) + row * a.ld + c;
-      load8(p, n, x);
-      if constexpr (KIND == kSwiglu) load8(p + cols, n, u);
+      d.x.load(p, n);
+      if constexpr (KIND == kSwiglu) d.u.load(p + cols, n);
     }
+    return d;
+  }, [&](int64_t row, int64_t c, const Data& r) {
+    const int64_t n = cols - c;
+    if (n <= 0) return;
+    float x[8], u[8], d[8], o[8], dx[8], du[8];
+    r.d.get(d);
+    r.x.get(x);
+    if constexpr (KIND == kSwiglu) r.u.get(u);
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
       if constexpr (KIND == kSwiglu) {
@@ -221,13 +308,21 @@ __global__ __launch_bounds__(kRowThreads) void activation_grad_kernel(BlockWalk 
 // Root-mean-square norm
 // ---------------------------------------------------------------------------
 // NT lanes share a row and hold it in registers, C times eight elements each:
-// a wave for rows of up to 2048 columns (four rows to a workgroup, no
+// a wave for rows of up to 1536 columns (four rows to a workgroup, no
 // barrier), 256 or 1024 threads for longer ones. A team walks rows with the
 // stride of the grid, so that the weights are read once a team.
+// (by lane rotations within 16 lanes, then one value of each 16: no LDS)
+template <int CTRL>
+__device__ __forceinline__ float dpp_add(float v) {
+  return v + __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, 0xF, 0xF, true));
+}
 __device__ __forceinline__ float wave_sum(float v) {
-#pragma unroll
-  for (int off = 32; off >= 1; off >>= 1) v += __shfl_xor(v, off, 64);
-  return v;
+  v = dpp_add<0x128>(v);
+  v = dpp_add<0x124>(v);
+  v = dpp_add<0x122>(v);
+  v = dpp_add<0x121>(v);
+  auto lane = [&](int l) { return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), l)); };
+  return (lane(0) + lane(16)) + (lane(32) + lane(48));
 }
 
 // Sum over the NT lanes of a team, in all of them, in a fixed order. `red` is
@@ -250,7 +345,7 @@ template <typename T, int NT, int C>
 __global__ __launch_bounds__(team_threads<NT>()) void rmsnorm_kernel(NormArgs a) {
   constexpr int kTeams = team_threads<NT>() / NT;
   __shared__ float red[2][16];
-  const int lane = threadIdx.x % NT, team = threadIdx.x / NT;
+  const int lane = threadIdx.x % NT, team = __builtin_amdgcn_readfirstlane(threadIdx.x / NT);
   const int cols = a.cols;
   float w[C][8];
 #pragma unroll
@@ -261,17 +356,22 @@ __global__ __launch_bounds__(team_threads<NT>()) void rmsnorm_kernel(NormArgs a)
   int parity = 0;
   for (int64_t row = int64_t(blockIdx.x) * kTeams + team; row < a.rows; row += int64_t(gridDim.x) * kTeams) {
     float v[C][8];
+    Raw<T> x[C], r[C];
+#pragma unroll
+    for (int i = 0; i < C; ++i) {
+      const int c = (lane + i * NT) * 8, n = cols - c;
+      x[i].load(static_cast<const T*>(a.x.data) + row * a.x.ld + c, n);
+      if (a.residual.data) r[i].load(static_cast<const T*>(a.residual.data) + row * a.residual.ld + c, n);
+    }
     float ss = 0.0f;
 #pragma unroll
     for (int i = 0; i < C; ++i) {
       const int c = (lane + i * NT) * 8, n = cols - c;
-      load8(static_cast<const T*>(a.x.data) + row * a.x.ld + c, n, v[i]);
+      x[i].get(v[i]);
       if (a.residual.data) {
-        float r[8];
-        load8(static_cast<const T*>(a.residual.data) + row * a.residual.ld + c, n, r);
         // rounded as it is stored: the backward pass sees the same stream
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[i][j] = float(T(v[i][j] + r[j]));
+        for (int j = 0; j < 8; ++j) v[i][j] = float(T(v[i][j] + float(r[i].v[j])));
         if (a.sum.data) store8(static_cast<T*>(a.sum.data) + row * a.sum.ld + c, n, v[i]);
       }
 #pragma unroll
@@ -303,7 +403,7 @@ __global__ __launch_bounds__(team_threads<NT>()) void rmsnorm_grad_kernel(NormAr
   constexpr int kTeams = team_threads<NT>() / NT;
   __shared__ float red[2][16];
   __shared__ float sums[kTeams > 1 ? (kTeams - 1) * NT * C * 8 : 1];
-  const int lane = threadIdx.x % NT, team = threadIdx.x / NT;
+  const int lane = threadIdx.x % NT, team = __builtin_amdgcn_readfirstlane(threadIdx.x / NT);
   const int cols = a.cols;
   float w[C][8], dw[C][8];
 #pragma unroll
@@ -316,20 +416,27 @@ __global__ __launch_bounds__(team_threads<NT>()) void rmsnorm_grad_kernel(NormAr
   int parity = 0;
   for (int64_t row = int64_t(blockIdx.x) * kTeams + team; row < a.rows; row += int64_t(gridDim.x) * kTeams) {
     const float rstd = a.rstd[row];
-    float h[C][8], d[C][8];
-    float dot = 0.0f;
+    // (kept as loaded and converted twice: half the registers of the values)
+    std::conditional_t<KEPT, RawCodes<>, Raw<T>> h[C];
+    Raw<T> d[C], r[C];
 #pragma unroll
     for (int i = 0; i < C; ++i) {
       const int c = (lane + i * NT) * 8, n = cols - c;
-      if constexpr (KEPT) get8(a.kept, row, c < cols ? c : 0, n, h[i]);
-      else load8(static_cast<const T*>(a.s.data) + row * a.s.ld + c, n, h[i]);
-      load8(static_cast<const T*>(a.dy.data) + row * a.dy.ld + c, n, d[i]);
+      if constexpr (KEPT) h[i].load(a.kept, row, c, n);
+      else h[i].load(static_cast<const T*>(a.s.data) + row * a.s.ld + c, n);
+      d[i].load(static_cast<const T*>(a.dy.data) + row * a.dy.ld + c, n);
+      if (a.residual_grad.data) r[i].load(static_cast<const T*>(a.residual_grad.data) + row * a.residual_grad.ld + c, n);
+    }
+    float dot = 0.0f;
+#pragma unroll
+    for (int i = 0; i < C; ++i) {
+      float x[8];
+      h[i].get(x);
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        h[i][j] *= rstd;
-        dw[i][j] = fmaf(d[i][j], h[i][j], dw[i][j]);
-        d[i][j] *= w[i][j];
-        dot = fmaf(d[i][j], h[i][j], dot);
+        const float p = float(d[i].v[j]) * (x[j] * rstd);
+        dw[i][j] += p;
+        dot = fmaf(p, w[i][j], dot);
       }
     }
     if (a.dx.data) {
@@ -338,11 +445,12 @@ __global__ __launch_bounds__(team_threads<NT>()) void rmsnorm_grad_kernel(NormAr
 #pragma unroll
       for (int i = 0; i < C; ++i) {
         const int c = (lane + i * NT) * 8, n = cols - c;
-        float r[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-        if (a.residual_grad.data) load8(static_cast<const T*>(a.residual_grad.data) + row * a.residual_grad.ld + c, n, r);
+        float x[8], o[8];
+        h[i].get(x);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) r[j] = fmaf(rstd, fmaf(-h[i][j], dot, d[i][j]), r[j]);
-        store8(static_cast<T*>(a.dx.data) + row * a.dx.ld + c, n, r);
+        for (int j = 0; j < 8; ++j)
+          o[j] = fmaf(rstd, fmaf(-(x[j] * rstd), dot, float(d[i].v[j]) * w[i][j]), a.residual_grad.data ? float(r[i].v[j]) : 0.0f);
+        store8(static_cast<T*>(a.dx.data) + row * a.dx.ld + c, n, o);
       }
     }
   }
@@ -411,7 +519,8 @@ template <class F>
 void with_team(int cols, F f) {
   if (cols <= 512) f(Int<64>(), Int<1>());
   else if (cols <= 1024) f(Int<64>(), Int<2>());
-  else if (cols <= 2048) f(Int<64>(), Int<4>());
+  else if (cols <= 1536) f(Int<64>(), Int<3>());
+  else if (cols <= 2048) f(Int<256>(), Int<1>());
   else if (cols <= 4096) f(Int<256>(), Int<2>());
   else if (cols <= 8192) f(Int<256>(), Int<4>());
   else f(Int<1024>(), Int<2>());
@@ -419,7 +528,7 @@ void with_team(int cols, F f) {
 
 // Workgroups of a norm: a row of the grid a team until every CU has eight.
 int64_t norm_groups(int64_t rows, int cols) {
-  const int64_t teams = cols <= 2048 ? 4 : 1;
+  const int64_t teams = cols <= 1536 ? 4 : 1;
   const int64_t all = (rows + teams - 1) / teams, most = cols <= 8192 ? 2048 : 512;
   return all < most ? all : most;
 }
