@@ -589,7 +589,6 @@ struct RowProduct {
   int rows, experts;
   int width, depth;                   // columns of the output, contraction
   int tiles_n;
-  int vec_out;                        // rows of the output start 16-byte aligned
 };
 
 template <typename T, int MB, class S, bool DA, bool DB>
@@ -652,7 +651,8 @@ __global__ __launch_bounds__(S::kThreads, S::kWorkgroups) void row_product_kerne
       const u32x4 v = *reinterpret_cast<const u32x4*>(st + r * (WN + 8) + c);
       T* p = out + int64_t(row) * g.ldc + col;
       if (col + 8 <= g.width) {
-        if (g.vec_out) *reinterpret_cast<u32x4*>(p) = v;
+        // (tiles of 64 columns a wave and more write whole lines)
+        if constexpr (WN >= 64) store16_nt(p, v);
         else __builtin_memcpy(p, &v, 16);
       } else {
 #pragma unroll
@@ -775,7 +775,9 @@ __global__ __launch_bounds__(S::kThreads, S::kWorkgroups) void weight_product_ke
 #pragma unroll
           for (int x = 0; x < 4; ++x) v[x] += t[x];
         }
-        __builtin_memcpy(p, v, 16);
+        u32x4 u;
+        __builtin_memcpy(&u, v, 16);
+        store16_nt(p, u);
       } else {
         for (int x = 0; x < 4; ++x)
           if (col + x < g.k) p[x] = add ? p[x] + v[x] : v[x];
@@ -959,7 +961,6 @@ void row_product(const GroupArgs& x, int width, int depth, hipStream_t stream) {
   g.experts = x.experts;
   g.width = width;
   g.depth = depth;
-  g.vec_out = aligned16(x.c) && x.ldc % 8 == 0;
   // copies straight to LDS need rows on 16 bytes, and a contraction in whole
   // chunks where an operand runs along it
   const bool da = aligned16(x.a) && x.lda % 8 == 0 && depth % 8 == 0;
