@@ -18,6 +18,7 @@
 // whose descriptor ends at the last valid row, so what lies beyond reads as zero,
 // and lanes beyond the end of the contraction get an address outside.
 #include <algorithm>
+#include <type_traits>
 
 #include "grad_device.h"
 
@@ -208,7 +209,7 @@ template <typename T, int MA, int MB, class S, bool DA, bool DB>
 struct Tile {
   static constexpr int BM = S::BM, BN = S::BN, WM = S::WM, WN = S::WN, KS = S::KS, NB = S::NB, SUB = S::SUB, PRE = S::PRE;
   static constexpr int kWavesN = S::kWavesN, kWaves = S::kWaves, kThreads = S::kThreads;
-  static constexpr int kMI = WM / 32, kNI = WN / 32;
+  static constexpr int kModeOfB = MB, kMI = WM / 32, kNI = WN / 32;
   static constexpr int kStageA = BM * KS * 2, kStageBytes = (BM + BN) * KS * 2;
   static constexpr int kLds = NB * kStageBytes;
 
@@ -589,30 +590,20 @@ struct RowProduct {
   int rows, experts;
   int width, depth;                   // columns of the output, contraction
   int tiles_n;
+  int places, main;                   // CUs, workgroups for whole tiles
 };
 
-template <typename T, int MB, class S, bool DA, bool DB>
-__global__ __launch_bounds__(S::kThreads, S::kWorkgroups) void row_product_kernel(RowProduct g) {
-  using K = Tile<T, kRows, MB, S, DA, DB>;
-  constexpr int BM = S::BM, BN = S::BN, WM = S::WM, WN = S::WN;
+// One tile: rows row0 .. of expert `e`, whose rows end at `end`, columns from col0 on.
+template <typename T, class K>
+__device__ __forceinline__ void row_product_tile(const RowProduct& g, char* smem, int expert, int row0, int end, int col0) {
+  constexpr int BM = K::BM, BN = K::BN, WM = K::WM, WN = K::WN, MB = K::kModeOfB;
   constexpr int kStage = 32 * (WN + 8);         // elements of a wave's output staging
   static_assert(K::kWaves * kStage * 2 <= K::kLds, "staging fits");
-  __shared__ __align__(16) char smem[K::kLds];
-  // An XCD (every eighth workgroup) takes an eighth of the tiles that there
-  // are, neighbours that share operands in its L2.
-  const int tiles_m = count_groups(g.offsets, g.experts, g.rows, BM, 0);
-  const int tiles = tiles_m * g.tiles_n, each = (tiles + 7) / 8, turn = blockIdx.x / 8;
-  const int id = int(blockIdx.x % 8) * each + turn;
-  if (turn >= each || id >= tiles) return;
-  int tm, tn;
-  banded(id, tiles_m, g.tiles_n, &tm, &tn);
-  const Span t = find_group(g.offsets, g.experts, g.rows, BM, 0, tm);
-  const int col0 = tn * BN;
-  const T* w = static_cast<const T*>(g.b) + t.expert * g.b_stride;
+  const T* w = static_cast<const T*>(g.b) + expert * g.b_stride;
   Source a, b;
-  a.p = reinterpret_cast<const char*>(static_cast<const T*>(g.a) + t.row0 * g.lda);
+  a.p = reinterpret_cast<const char*>(static_cast<const T*>(g.a) + row0 * g.lda);
   a.ld = g.lda * 2;
-  a.rows = min(t.end - t.row0, BM);
+  a.rows = min(end - row0, BM);
   a.depth = g.depth;
   a.cols = 0;
   a.wide = g.depth >= 8;
@@ -646,8 +637,8 @@ __global__ __launch_bounds__(S::kThreads, S::kWorkgroups) void row_product_kerne
 #pragma unroll
     for (int q = 0; q < 32 * kPer / 64; ++q) {
       const int r = (q * 64 + lane) / kPer, c = (lane % kPer) * 8;
-      const int row = t.row0 + wm + 32 * i + r, col = col0 + wn + c;
-      if (row >= t.end || col >= g.width) continue;
+      const int row = row0 + wm + 32 * i + r, col = col0 + wn + c;
+      if (row >= end || col >= g.width) continue;
       const u32x4 v = *reinterpret_cast<const u32x4*>(st + r * (WN + 8) + c);
       T* p = out + int64_t(row) * g.ldc + col;
       if (col + 8 <= g.width) {
@@ -662,6 +653,41 @@ __global__ __launch_bounds__(S::kThreads, S::kWorkgroups) void row_product_kerne
     }
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
   }
+}
+
+// Q: quarters of S's tile. Tiles that would be a last round on at most half the CUs run as
+// four of them each, two to a CU if need be, in workgroups behind the others
+// (4096 x 1024 by 16384 rows: 16 of 272 tiles).
+template <typename T, int MB, class S, class Q, bool DA, bool DB>
+__global__ __launch_bounds__(S::kThreads, S::kWorkgroups) void row_product_kernel(RowProduct g) {
+  using K = Tile<T, kRows, MB, S, DA, DB>;
+  constexpr int BM = S::BM, BN = S::BN;
+  constexpr bool kTail = !std::is_void_v<Q>;
+  __shared__ __align__(16) char smem[K::kLds];
+  // An XCD (every eighth workgroup) takes an eighth of the tiles that there
+  // are, neighbours that share operands in its L2.
+  const int tiles_m = count_groups(g.offsets, g.experts, g.rows, BM, 0), tiles = tiles_m * g.tiles_n;
+  const int rest = kTail ? tiles % g.places : 0, tail = 2 * rest <= g.places ? rest : 0;
+  const bool behind = kTail && int(blockIdx.x) >= g.main;
+  const int number = behind ? blockIdx.x - g.main : blockIdx.x, turn = number / 8 / (behind ? 4 : 1);
+  const int count = behind ? tail : tiles - tail, each = (count + 7) / 8;
+  int id = number % 8 * each + turn;
+  if (turn >= each || id >= count) return;
+  if (behind) id += tiles - tail;
+  int tm, tn;
+  banded(id, tiles_m, g.tiles_n, &tm, &tn);
+  const Span t = find_group(g.offsets, g.experts, g.rows, BM, 0, tm);
+  if constexpr (kTail) {
+    if (behind) {
+      static_assert(Q::BM * 2 == BM && Q::BN * 2 == BN && Q::kThreads == S::kThreads, "quarters");
+      using KQ = Tile<T, kRows, MB, Q, DA, DB>;
+      static_assert(KQ::kLds <= K::kLds, "one block of LDS");
+      const int q = number / 8 % 4, row0 = t.row0 + (q >> 1) * Q::BM, col0 = tn * BN + (q & 1) * Q::BN;
+      if (row0 < t.end && col0 < g.width) row_product_tile<T, KQ>(g, smem, t.expert, row0, t.end, col0);
+      return;
+    }
+  }
+  row_product_tile<T, K>(g, smem, t.expert, t.row0, t.end, tn * BN);
 }
 
 // ---------------------------------------------------------------------------
@@ -863,9 +889,9 @@ constexpr TileCost kWeightTiles[3] = {{256, 128, 1, 0.7, 1.0, 6.0}, {128, 128, 2
 
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
-// Tile of a row product: the least time by rounds of tiles over the CUs. An
-// expert's last tile is half empty on average.
-int row_tile(int64_t rows, int64_t experts, int64_t width, int64_t depth, int cus) {
+// Tile of a row product: the least time by rounds of tiles over the CUs, the last one
+// in quarters where the kernel does that. An expert's last tile is half empty on average.
+int row_tile(int64_t rows, int64_t experts, int64_t width, int64_t depth, int cus, bool aligned) {
   int best = 0;
   double least = 0.0;
   for (int i = 0; i < 3; ++i) {
@@ -875,7 +901,8 @@ int row_tile(int64_t rows, int64_t experts, int64_t width, int64_t depth, int cu
     const int64_t places = int64_t(cus) * c.at_once, left = tiles % places;
     const double stages = double(ceil_div(depth, 64));
     double t = double(tiles / places) * (c.full * stages + c.rest);
-    if (left > 0) t += (left <= cus && i > 0 ? c.alone : left * 4 <= cus ? c.alone : c.full) * stages + c.rest;
+    if (i == 0 && aligned && left * 2 <= cus) t += left > 0 ? kRowTiles[1].alone * (left * 4 <= cus ? 1.0 : 1.5) * stages + c.rest : 0.0;
+    else if (left > 0) t += (left <= cus && i > 0 ? c.alone : left * 4 <= cus ? c.alone : c.full) * stages + c.rest;
     if (i == 0 || t < least) {
       best = i;
       least = t;
@@ -922,28 +949,30 @@ WeightPlan weight_plan(int64_t rows, int64_t experts, int64_t n, int64_t k, int 
 // Slots of partial sums that parts of that many rows can need.
 int64_t partial_slots(int64_t rows, int64_t part) { return part > rows ? 0 : 2 * rows / part + 1; }
 
-// S: shape where both operands are copied straight to LDS, R: otherwise.
-template <typename T, int MB, class S, class R>
+// S: shape where both operands are copied straight to LDS, with quarters Q; R: otherwise.
+template <typename T, int MB, class S, class Q, class R>
 void run_rows(RowProduct g, bool da, bool db, hipStream_t stream) {
   g.tiles_n = (g.width + S::BN - 1) / S::BN;
   // the most tiles that any split of the rows into experts makes
   const int64_t tiles = (int64_t(g.rows) / S::BM + std::min(g.experts, g.rows)) * g.tiles_n;
-  const dim3 grid(unsigned((tiles + 7) / 8 * 8));
+  g.main = int((tiles + 7) / 8 * 8);
   if (da && db) {
-    row_product_kernel<T, MB, S, true, true><<<grid, S::kThreads, 0, stream>>>(g);
+    const int64_t quarters = std::is_void_v<Q> ? 0 : (std::min<int64_t>(tiles, g.places / 2) + 7) / 8 * 32;
+    row_product_kernel<T, MB, S, Q, true, true><<<dim3(unsigned(g.main + quarters)), S::kThreads, 0, stream>>>(g);
     return;
   }
+  const dim3 grid(unsigned(g.main));
   if constexpr (MB == kCols) {       // (rows of Y = X W^T's operands are alike)
     if (db) {
-      row_product_kernel<T, MB, R, false, true><<<grid, R::kThreads, 0, stream>>>(g);
+      row_product_kernel<T, MB, R, void, false, true><<<grid, R::kThreads, 0, stream>>>(g);
       return;
     }
     if (da) {
-      row_product_kernel<T, MB, R, true, false><<<grid, R::kThreads, 0, stream>>>(g);
+      row_product_kernel<T, MB, R, void, true, false><<<grid, R::kThreads, 0, stream>>>(g);
       return;
     }
   }
-  row_product_kernel<T, MB, R, false, false><<<grid, R::kThreads, 0, stream>>>(g);
+  row_product_kernel<T, MB, R, void, false, false><<<grid, R::kThreads, 0, stream>>>(g);
 }
 
 template <typename T, int MB>
@@ -959,16 +988,17 @@ void row_product(const GroupArgs& x, int width, int depth, hipStream_t stream) {
   g.b_stride = x.b_stride;
   g.rows = int(x.rows);
   g.experts = x.experts;
+  g.places = x.cus;
   g.width = width;
   g.depth = depth;
   // copies straight to LDS need rows on 16 bytes, and a contraction in whole
   // chunks where an operand runs along it
   const bool da = aligned16(x.a) && x.lda % 8 == 0 && depth % 8 == 0;
   const bool db = aligned16(x.b) && x.ldb % 8 == 0 && x.b_stride % 8 == 0 && (MB == kCols || depth % 8 == 0);
-  switch (row_tile(x.rows, x.experts, width, depth, x.cus)) {
-    case 0: run_rows<T, MB, Shape<256, 256, 128, 64, 64, 2, 2>, Shape<256, 256, 128, 64, 64, 2, 1>>(g, da, db, stream); break;
-    case 1: run_rows<T, MB, Shape<128, 128, 64, 64, 64, 2, 2>, Shape<128, 128, 64, 64, 64, 2, 1, 2>>(g, da, db, stream); break;
-    default: run_rows<T, MB, Shape<64, 64, 32, 32, 64, 4, 4>, Shape<64, 64, 32, 32, 64, 4, 4, 4>>(g, da, db, stream); break;
+  switch (row_tile(x.rows, x.experts, width, depth, x.cus, da && db)) {
+    case 0: run_rows<T, MB, Shape<256, 256, 128, 64, 64, 2, 2>, Shape<128, 128, 64, 32, 64, 2, 2>, Shape<256, 256, 128, 64, 64, 2, 1>>(g, da, db, stream); break;
+    case 1: run_rows<T, MB, Shape<128, 128, 64, 64, 64, 2, 2>, void, Shape<128, 128, 64, 64, 64, 2, 1, 2>>(g, da, db, stream); break;
+    default: run_rows<T, MB, Shape<64, 64, 32, 32, 64, 4, 4>, void, Shape<64, 64, 32, 32, 64, 4, 4, 4>>(g, da, db, stream); break;
   }
 }
 
