@@ -502,8 +502,8 @@ struct Tile {
 #pragma unroll
       for (int m = 0; m < kMfmas; ++m) {
         const int u = m / (kMI * kNI), i = m / kNI % kMI, j = m % kNI;
-        if constexpr (FOLD > 0) acc[i][j] = mma(fa[cur][u * kMI + i], fb[cur][u * kNI + j], acc[i][j], T());
-        else out[i][j] = mma(fa[cur][u * kMI + i], fb[cur][u * kNI + j], out[i][j], T());
+        if constexpr (FOLD > 0) acc[i][j] = mma(fb[cur][u * kNI + j], fa[cur][u * kMI + i], acc[i][j], T());
+        else out[i][j] = mma(fb[cur][u * kNI + j], fa[cur][u * kMI + i], out[i][j], T());
 #pragma unroll
         for (int f = m * kFrags / kMfmas; f < (m + 1) * kFrags / kMfmas; ++f) read(cur ^ 1, buf1, st1, f);
         // what comes through registers first: the wait for it would include
@@ -617,8 +617,9 @@ __device__ __forceinline__ void row_product_tile(const RowProduct& g, char* smem
   K::template product<0>(a, b, typename K::CodeSource{}, g.depth, smem, acc);
   lds_barrier();
   // Output through LDS, 32 rows of a wave at a time: rows of 16-bit values
-  // leave as whole 16-byte pieces. Element r of a block is row
-  // 8 (r / 4) + 4 (lane / 32) + r % 4, column lane % 32.
+  // leave as whole 16-byte pieces. Element r of a block is row lane % 32, column
+  // 8 (r / 4) + 4 (lane / 32) + r % 4 (B is the matrix unit's first operand, so
+  // that a lane has four columns in a row: an LDS write each).
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wm = (wave / K::kWavesN) * WM, wn = (wave % K::kWavesN) * WN;
@@ -629,8 +630,14 @@ __device__ __forceinline__ void row_product_tile(const RowProduct& g, char* smem
 #pragma unroll
     for (int j = 0; j < K::kNI; ++j)
 #pragma unroll
-      for (int r = 0; r < 16; ++r)
-        st[(8 * (r >> 2) + 4 * (lane >> 5) + (r & 3)) * (WN + 8) + 32 * j + (lane & 31)] = T(acc[i][j][r]);
+      for (int r = 0; r < 4; ++r) {
+        T v[4];
+#pragma unroll
+        for (int x = 0; x < 4; ++x) v[x] = T(acc[i][j][4 * r + x]);
+        u32x2 u;
+        __builtin_memcpy(&u, v, 8);
+        *reinterpret_cast<u32x2*>(st + (lane & 31) * (WN + 8) + 32 * j + 8 * r + 4 * (lane >> 5)) = u;
+      }
     // (a wave's own region: its LDS accesses are in order)
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     constexpr int kPer = WN / 8;
@@ -782,7 +789,9 @@ __global__ __launch_bounds__(S::kThreads, S::kWorkgroups) void weight_product_ke
 #pragma unroll
     for (int j = 0; j < K::kNI; ++j)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) st[(8 * (r >> 2) + 4 * (lane >> 5) + (r & 3)) * kLd + 32 * j + (lane & 31)] = acc[q][j][r];
+      for (int r = 0; r < 4; ++r)
+        *reinterpret_cast<f32x4*>(st + (lane & 31) * kLd + 32 * j + 8 * r + 4 * (lane >> 5)) =
+            f32x4{acc[q][j][4 * r], acc[q][j][4 * r + 1], acc[q][j][4 * r + 2], acc[q][j][4 * r + 3]};
     // (a wave's own region: its LDS accesses are in order)
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     constexpr int kPer = WN / 4;
