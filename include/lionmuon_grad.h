@@ -75,7 +75,9 @@ typedef struct lm_stack {
 } lm_stack;
 
 /* 8-bit checkpoint of rows x cols values (format above). scales holds
- * ceil(cols / LM_CHECKPOINT_BLOCK) bytes a row, rows ld_scales bytes apart. */
+ * ceil(cols / LM_CHECKPOINT_BLOCK) bytes a row, rows ld_scales bytes apart; where
+ * ld_scales is a multiple of 4, all rows * ld_scales bytes can be read (the
+ * weight gradient then copies scales four at a time, and is faster). */
 typedef struct lm_checkpoint {
   void* codes;
   void* scales;

@@ -76,6 +76,13 @@ __device__ __forceinline__ void copy16(u32x4 desc, uint32_t off, uint32_t dst) {
   asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds"
                :: "v"(off), "s"(u), "s"(__builtin_amdgcn_readfirstlane(dst)) : "memory", "m0");
 }
+// 4 bytes a lane, at dst + 4 i.
+__device__ __forceinline__ void copy4(u32x4 desc, uint32_t off, uint32_t dst) {
+  const u32x4 u = {uint32_t(__builtin_amdgcn_readfirstlane(desc[0])), uint32_t(__builtin_amdgcn_readfirstlane(desc[1])),
+                   uint32_t(__builtin_amdgcn_readfirstlane(desc[2])), 0x00027000u};
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dword %0, %1, 0 offen lds"
+               :: "v"(off), "s"(u), "s"(__builtin_amdgcn_readfirstlane(dst)) : "memory", "m0");
+}
 __device__ __forceinline__ uint32_t lds_address(const void* p) {
   return uint32_t(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) const char*)(p)));
 }
@@ -210,8 +217,12 @@ struct Tile {
   static constexpr int BM = S::BM, BN = S::BN, WM = S::WM, WN = S::WN, KS = S::KS, NB = S::NB, SUB = S::SUB, PRE = S::PRE;
   static constexpr int kWavesN = S::kWavesN, kWaves = S::kWaves, kThreads = S::kThreads;
   static constexpr int kModeOfB = MB, kMI = WM / 32, kNI = WN / 32;
-  static constexpr int kStageA = BM * KS * 2, kStageBytes = (BM + BN) * KS * 2;
-  static constexpr int kLds = NB * kStageBytes;
+  // Codes that go straight to LDS (DB) lie there as they are, each wave's scales
+  // behind them; what they stand for is put into one of two more buffers.
+  static constexpr bool kRaw = MB == kCodes && DB;
+  static constexpr int kStageA = BM * KS * 2, kStageB = BN * KS * 2;
+  static constexpr int kStageBytes = kStageA + (kRaw ? BN * KS + kWaves * 256 : kStageB);
+  static constexpr int kLds = NB * kStageBytes + (kRaw ? 2 * kStageB : 0);
 
   // Copies of one operand's stages (16-bit operands), by DMA: kInst copies of a
   // wave for each stage of 64 contraction values.
@@ -355,6 +366,50 @@ struct Tile {
     *reinterpret_cast<u32x4*>(dst + row * (BN * 2) + (c ^ Stage<kCols, BN, KS>::swz(row)) * 16) = o;
   }
 
+  // The same by DMA: one copy of codes and one of scales a wave and stage, both of
+  // the 16 codes of a row that the lane itself converts.
+  struct CodeCopier {
+    const CodeSource& s;
+    u32x4 dc, ds;
+    uint32_t oc, os, shift;
+    int wave;
+    __device__ __forceinline__ CodeCopier(const CodeSource& src, int w, int lane) : s(src), wave(w) {
+      static_assert(BN * KS == kThreads * 16, "16 codes a thread");
+      constexpr int kPer = BN / 16;
+      const int i = w * 64 + lane, row = i / kPer;
+      oc = uint32_t(row) * uint32_t(s.ld) + i % kPer * 16;
+      os = uint32_t(row) * uint32_t(s.lds);
+      shift = (reinterpret_cast<uintptr_t>(s.scales) & 3) * 8;
+    }
+    __device__ __forceinline__ void start(int k0) {
+      const int left = min(s.depth - k0, KS);
+      dc = descriptor(s.codes + int64_t(k0) * s.ld, left > 0 ? (left - 1) * s.ld + (int64_t(s.cols) + 15) / 16 * 16 : 0);
+      ds = descriptor(s.scales + int64_t(k0) * s.lds - shift / 8, left > 0 ? (left - 1) * s.lds + 4 : 0);
+    }
+    __device__ __forceinline__ void copy(int q, uint32_t dst) const {      // dst: LDS address of the codes
+      if (q == 0) copy16(dc, oc, dst + wave * 1024);
+      else copy4(ds, os, dst + BN * KS + wave * 256);
+    }
+    // from codes at `src` to bf16 at `dst`
+    __device__ __forceinline__ void convert(const char* src, char* dst, int lane) const {
+      constexpr int kPer = BN / 16;
+      const int i = wave * 64 + lane, row = i / kPer;
+      const u32x4 v = *reinterpret_cast<const u32x4*>(src + i * 16);
+      const uint32_t e = *reinterpret_cast<const uint32_t*>(src + BN * KS + i * 4);
+      const float scale = scale_of((e >> shift) & 0xffu);
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        u32x4 o;
+#pragma unroll
+        for (int w = 0; w < 2; ++w) {
+          o[2 * w] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(v[2 * h + w], scale, false));
+          o[2 * w + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(v[2 * h + w], scale, true));
+        }
+        *reinterpret_cast<u32x4*>(dst + row * (BN * 2) + ((i % kPer * 2 + h) ^ Stage<kCols, BN, KS>::swz(row)) * 16) = o;
+      }
+    }
+  };
+
   // Fragment of 32 rows (or columns) from `w0` on and contraction values
   // 16 kk .. + 15 of a stage: lane l holds row l % 32, values 8 (l / 32) .. + 7.
   template <int MODE, int W>
@@ -395,12 +450,15 @@ struct Tile {
     const int wm = (wave / kWavesN) * WM, wn = (wave % kWavesN) * WN;
     const int nk = (depth + KS - 1) / KS;
     constexpr int kModeB = MB == kCodes ? int(kCols) : MB;
-    static_assert(!(DB && MB == kCodes), "codes go through registers");
-    constexpr int kCopiesA = DA ? Copier<MA, BM>::kInst : 0, kCopiesB = DB ? Copier<kModeB, BN>::kInst : 0;
+    constexpr int kCopiesA = DA ? Copier<MA, BM>::kInst : 0, kCopiesB = kRaw ? 2 : DB ? Copier<kModeB, BN>::kInst : 0;
     constexpr int kCopies = kCopiesA + kCopiesB;
-    constexpr int kPiecesB = MB == kCodes ? kPieces : 0;
+    constexpr int kPiecesB = MB == kCodes && !kRaw ? kPieces : 0;
+    static_assert(!kRaw || (DA && NB == 3 && KS / 16 / SUB == 2), "the waits below");
     Copier<MA, BM> ca(a, wave, lane);
-    Copier<kModeB, BN> cb(b, wave, lane);
+    std::conditional_t<kRaw, CodeCopier, Copier<kModeB, BN>> cb = [&] {
+      if constexpr (kRaw) return CodeCopier(c, wave, lane);
+      else return Copier<kModeB, BN>(b, wave, lane);
+    }();
     Regs<MA, DA ? 0 : BM> ra[PRE];
     Regs<kModeB, (DB || MB == kCodes) ? 0 : BN> rb[PRE];
     CodeRegs rc[PRE];
@@ -411,7 +469,7 @@ struct Tile {
       if constexpr (!DB && MB != kCodes) fetch<kModeB, BN>(b, kt * KS, tid, rb[set]);
     };
     auto load_codes = [&](int kt, int set) {
-      if constexpr (MB == kCodes) fetch(c, kt * KS, tid, rc[set]);
+      if constexpr (kPiecesB > 0) fetch(c, kt * KS, tid, rc[set]);
     };
     constexpr int kWritesA = DA ? 0 : Regs<MA, BM>::kInst, kWritesB = (DB || MB == kCodes) ? 0 : Regs<kModeB, BN>::kInst;
     constexpr int kWrites = kWritesA + kWritesB;
@@ -431,13 +489,18 @@ struct Tile {
     };
     const uint32_t lds = lds_address(smem) + wave * 1024;
     auto copy = [&](int q, int buf) {              // buf: byte offset of a stage's buffer
+      if constexpr (kRaw) {                        // codes first: they are needed first
+        if (q < kCopiesB) cb.copy(q, lds_address(smem) + buf + kStageA);
+        else ca.copy(q - kCopiesB, lds + buf);
+        return;
+      }
       if constexpr (DA) {
         if (q < kCopiesA) {
           ca.copy(q, lds + buf);
           return;
         }
       }
-      if constexpr (DB) cb.copy(q - kCopiesA, lds + buf + kStageA);
+      if constexpr (DB && !kRaw) cb.copy(q - kCopiesA, lds + buf + kStageA);
     };
     f32x16 acc[FOLD ? kMI : 1][FOLD ? kNI : 1];
     auto zero = [](auto& x) {
@@ -447,7 +510,7 @@ struct Tile {
     zero(out);
     if (nk == 0) return;
     // the slots' pattern repeats after kTurns stages
-    constexpr int kTurns = PRE > 1 ? (PRE % 2 == 0 ? PRE : 2 * PRE) : KS / 16 / SUB % 2 == 0 ? 1 : 2;
+    constexpr int kTurns = PRE > 1 ? (PRE % 2 == 0 ? PRE : 2 * PRE) : KS / 16 / SUB % 2 == 0 && !kRaw ? 1 : 2;
     constexpr int kSteps = KS / 16 / SUB, kFrags = SUB * (kMI + kNI), kMfmas = SUB * kMI * kNI;
     // A stage's copies start in the last step of stage kt - NB, and, with more than
     // two buffers, which leave them time to land, go on through that of the next
@@ -484,28 +547,35 @@ struct Tile {
       }
     }
     if constexpr (kCopies > 0) wait_vmcnt<(NB - 2) * kCopies + kFirst>();
+    char* const wide = smem + NB * kStageBytes;    // kRaw: two buffers of B's values
+    if constexpr (kRaw) cb.convert(smem + kStageA, wide, lane);
     lds_barrier();
     s16x8 fa[2][SUB * kMI], fb[2][SUB * kNI];
     // fragment f of step st of the stage at buf: of each 16 values A's blocks, then B's
-    auto read = [&](int slot, int buf, int st, int f) {
+    auto read = [&](int slot, int buf, int par, int st, int f) {
       const int u = f / (kMI + kNI), g = f % (kMI + kNI);
-      const char* p = smem + buf;
+      const char *p = smem + buf, *pb = kRaw ? wide + par * kStageB : p + kStageA;
       if (g < kMI) fa[slot][u * kMI + g] = fragment<MA, BM>(p, wm + 32 * g, st * SUB + u, lane);
-      else fb[slot][u * kNI + g - kMI] = fragment<kModeB, BN>(p + kStageA, wn + 32 * (g - kMI), st * SUB + u, lane);
+      else fb[slot][u * kNI + g - kMI] = fragment<kModeB, BN>(pb, wn + 32 * (g - kMI), st * SUB + u, lane);
     };
 #pragma unroll
-    for (int f = 0; f < kFrags; ++f) read(0, 0, 0, f);
+    for (int f = 0; f < kFrags; ++f) read(0, 0, 0, 0, f);
     // One step (fragments in slot `cur`): its MFMAs, each followed by its share of the
     // next step's reads (step st1 of the stage at buf1), of copies q0 .. q1 to
     // `fill` and, in the last step, of the writes to it.
-    auto step = [&](int cur, int buf1, int st1, int fill, int q0, int q1, bool last, int kt, int set) {
+    auto step = [&](int cur, int buf1, int par1, int st1, int fill, int q0, int q1, bool last, int kt, int set) {
 #pragma unroll
       for (int m = 0; m < kMfmas; ++m) {
         const int u = m / (kMI * kNI), i = m / kNI % kMI, j = m % kNI;
         if constexpr (FOLD > 0) acc[i][j] = mma(fb[cur][u * kNI + j], fa[cur][u * kMI + i], acc[i][j], T());
         else out[i][j] = mma(fb[cur][u * kNI + j], fa[cur][u * kMI + i], out[i][j], T());
 #pragma unroll
-        for (int f = m * kFrags / kMfmas; f < (m + 1) * kFrags / kMfmas; ++f) read(cur ^ 1, buf1, st1, f);
+        for (int f = m * kFrags / kMfmas; f < (m + 1) * kFrags / kMfmas; ++f) read(cur ^ 1, buf1, par1, st1, f);
+        // kRaw: the next stage's codes, in the first step
+        if constexpr (kRaw) {
+          if (!last && m == kMfmas / 4)
+            cb.convert(smem + (buf1 == (NB - 1) * kStageBytes ? 0 : buf1 + kStageBytes) + kStageA, wide + (par1 ^ 1) * kStageB, lane);
+        }
         // what comes through registers first: the wait for it would include
         // copies that have just been started
         constexpr int kParts = kPiecesB + kWrites == 0 ? 0 : kCopies == 0 || kMfmas == 1 ? kMfmas : kMfmas / 2;
@@ -529,10 +599,13 @@ struct Tile {
     auto stage = [&](int kt, int turn) {           // turn: kt modulo kTurns
       const int par = turn * kSteps, set = turn % PRE;
       const int next = buf == (NB - 1) * kStageBytes ? 0 : buf + kStageBytes;
+      // this wave's codes of the next stage have landed: the copies started after
+      // them are that stage's others and the first ones of the stage behind it
+      if constexpr (kRaw) wait_vmcnt<kCopies - 2 + kFirst>();
 #pragma unroll
       for (int st = 0; st + 1 < kSteps; ++st) {
         constexpr int kLeft = kCopies - kFirst, kOver = kSteps > 1 ? kSteps - 1 : 1;
-        step((par + st) & 1, buf, st + 1, filling, kFirst + st * kLeft / kOver, kFirst + (st + 1) * kLeft / kOver, false, 0, 0);
+        step((par + st) & 1, buf, turn & 1, st + 1, filling, kFirst + st * kLeft / kOver, kFirst + (st + 1) * kLeft / kOver, false, 0, 0);
       }
       // stage kt + 1 has landed: at least that many copies of later ones
       // were started after its own
@@ -540,7 +613,7 @@ struct Tile {
       lds_barrier();
       start(kt + NB);
       __builtin_amdgcn_sched_barrier(0);
-      step((par + kSteps - 1) & 1, next, 0, buf, 0, kFirst, true, kt + NB, set);
+      step((par + kSteps - 1) & 1, next, (turn & 1) ^ 1, 0, buf, 0, kFirst, true, kt + NB, set);
       // (the registers are free now)
       if (kt + NB + PRE < nk) load(kt + NB + PRE, set);
       load_codes(kt + NB + PRE, set);
@@ -1020,6 +1093,12 @@ void run_weight(WeightProduct g, bool da, bool db, hipStream_t stream) {
   g.chunk = int((per + 7) / 8);
   const dim3 grid(grid_of(per * (g.rows / g.part + g.experts), g.chunk));
   if constexpr (MB == kCodes) {
+    if constexpr (S::BN * S::KS == S::kThreads * 16 && S::NB == 3) {
+      if (da && db) {
+        weight_product_kernel<T, MB, S, true, true><<<grid, S::kThreads, 0, stream>>>(g);
+        return;
+      }
+    }
     if (da) weight_product_kernel<T, MB, R, true, false><<<grid, R::kThreads, 0, stream>>>(g);
     else weight_product_kernel<T, MB, R, false, false><<<grid, R::kThreads, 0, stream>>>(g);
   } else {
@@ -1050,7 +1129,9 @@ void weight_product(const GroupArgs& x, hipStream_t stream) {
   g.k = x.k;
   g.accumulate = x.accumulate;
   g.part = int(plan.part);
-  const bool da = aligned16(x.a) && x.lda % 8 == 0, db = MB != kCodes && aligned16(x.b) && x.ldb % 8 == 0;
+  const bool da = aligned16(x.a) && x.lda % 8 == 0;
+  // (scales are copied four at a time, from multiples of four bytes)
+  const bool db = MB == kCodes ? reinterpret_cast<uintptr_t>(x.kept.scales) % 4 == 0 && x.kept.ld_scales % 4 == 0 : aligned16(x.b) && x.ldb % 8 == 0;
   switch (plan.tile) {
     case 0: run_weight<T, MB, Shape<256, 128, 64, 64, 64, 3, 2>, Shape<256, 128, 64, 64, 64, 3, 1>>(g, da, db, stream); break;
     case 1: run_weight<T, MB, Shape<128, 128, 64, 64, 64, 2, 1>, Shape<128, 128, 64, 64, 64, 2, 1>>(g, da, db, stream); break;

@@ -110,6 +110,9 @@ class Checkpoint:
         ld_scales, step_scales = scales.stride()
         if (cols > 1 and step != 1) or (blocks > 1 and step_scales != 1):
             _invalid("the rows of codes and scales must be contiguous")
+        if ld_scales % 4 == 0 and rows * ld_scales > \
+                scales.untyped_storage().nbytes() - scales.storage_offset():
+            _invalid("the last row of scales must be as long as the others")
         self.shape = codes.shape
         self.device = codes.device
         self._buffer = None
@@ -124,13 +127,15 @@ class Checkpoint:
         """An uninitialised checkpoint (filled by the operators that write one):
         its codes and scales lie in one allocation."""
         ld, blocks = -(-cols // 16) * 16, -(-cols // CHECKPOINT_BLOCK)
+        ld_scales = -(-blocks // 4) * 4
         self = cls.__new__(cls)
-        self._buffer = buffer = torch.empty(rows * (ld + blocks), dtype=torch.uint8, device=device)
+        self._buffer = buffer = torch.empty(rows * (ld + ld_scales), dtype=torch.uint8, device=device)
         self.shape = torch.Size((rows, cols))
         self.device = buffer.device
         self._codes = self._scales = None
         base = buffer.data_ptr()
-        self._desc = lm_checkpoint(base, base + rows * ld if base else 0, rows, cols, ld, blocks)
+        self._desc = lm_checkpoint(base, base + rows * ld if base else 0, rows, cols, ld,
+                                   ld_scales)
         return self
 
     @property
@@ -143,8 +148,9 @@ class Checkpoint:
     @property
     def scales(self):
         if self._scales is None:
-            rows, d = self._desc.rows, self._desc
-            self._scales = self._buffer[rows * d.ld_codes:].view(rows, d.ld_scales)
+            rows, cols, d = self._desc.rows, self._desc.cols, self._desc
+            self._scales = self._buffer[rows * d.ld_codes:].view(rows, d.ld_scales)[
+                :, :-(-cols // CHECKPOINT_BLOCK)]
         return self._scales
 
 

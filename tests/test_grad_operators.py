@@ -540,3 +540,53 @@ def test_captured_layer_replays_with_new_inputs():
         for g, static, out in graphs:
             for x, y in zip(out, want):
                 assert torch.equal(x, y)
+
+
+# -- large tiles -------------------------------------------------------------
+def gpu_products(call, a, w, at, transpose):
+    """float64 products on the GPU, rows of no expert 0."""
+    y = torch.zeros(a.shape[0], w.shape[2] if transpose else w.shape[1], dtype=torch.float64, device="cuda")
+    for e in range(w.shape[0]):
+        r = slice(int(at[e]), int(at[e + 1]))
+        y[r] = a[r].double() @ (w[e].double() if transpose else w[e].double().t())
+    return y
+
+
+# the largest tiles, a last round in quarters (4200 x 4100: 17 x 17 tiles of 256), and
+# operands off 16 bytes at either side
+@pytest.mark.parametrize("experts,rows,n,k,pad", [(1, 4200, 4100, 512, 0), (3, 4300, 4096, 264, 0), (2, 4000, 2051, 776, 0),
+                                                  (2, 4000, 776, 2051, 0), (2, 3000, 1100, 1500, 1)])
+def test_large_products(experts, rows, n, k, pad):
+    dt = torch.bfloat16
+    x, dy, w, offsets, at = group(rows, experts, n, k, dt, 31, tail=5, pad=pad, off=pad)
+    inside = slice(0, int(at[-1]))
+    for call, a, depth, transpose in ((gr.lionmuon_grouped_product, x, k, False),
+                                      (gr.lionmuon_grouped_input_grad, dy, n, True)):
+        want = gpu_products(call, a, w, at, transpose)
+        out = torch.full(want.shape, 7.0, dtype=dt, device="cuda")
+        call(a, w, offsets, out=out)
+        # independent terms of mean square v: a sum of `depth` is off by at most depth v^0.5 times
+        # the roundings of sum_bound, and by half a step of its own
+        v = float(a[inside].double().square().mean() * w.double().square().mean()) ** 0.5
+        err = (out[inside].double() - want[inside]).abs()
+        assert (err <= half_step(dt) * 1.01 * want[inside].abs() + sum_bound(depth) * depth * v).all()
+        assert (out[int(at[-1]):] == 7.0).all()
+
+
+@pytest.mark.parametrize("experts,rows,n,k", [(1, 5000, 512, 1280), (3, 9000, 700, 640), (2, 700, 2560, 1152),
+                                              (1, 70, 256, 128), (1, 20000, 300, 1000)])
+def test_weight_gradient_from_a_checkpoint_is_that_of_its_values(experts, rows, n, k):
+    x, dy, _, offsets, at = group(rows, experts, n, k, torch.bfloat16, 41, tail=3)
+    kept = gr.lionmuon_checkpoint(x)
+    same = gr.lionmuon_checkpoint_restore(kept)
+    got = gr.lionmuon_grouped_weight_grad(dy, kept, offsets)
+    assert torch.equal(got, gr.lionmuon_grouped_weight_grad(dy, same, offsets))
+    want = torch.stack([dy[at[e]:at[e + 1]].double().t() @ same[at[e]:at[e + 1]].double() for e in range(experts)])
+    for e in range(experts):
+        if at[e + 1] > at[e]:
+            assert float((got[e].double() - want[e]).norm() / want[e].norm()) < 1e-6
+    # scales that cannot be copied four at a time give the same
+    wide = torch.zeros(kept.scales.shape[0], kept.scales.shape[1] + 5, dtype=torch.uint8, device="cuda")
+    wide[:, 1:1 + kept.scales.shape[1]] = kept.scales
+    odd = gr.Checkpoint(kept.codes, wide[:, 1:1 + kept.scales.shape[1]])
+    assert float((gr.lionmuon_grouped_weight_grad(dy, odd, offsets) - got).norm() / got.norm()) < 1e-6
