@@ -27,6 +27,9 @@ struct CkptView {
 
 constexpr int kCkptBlock = 128;
 
+// Workgroups of a launch at most: with 512 threads each, 2^31 threads.
+constexpr int64_t kMaxWorkgroups = int64_t(1) << 22;
+
 hipError_t launch_checkpoint(Elem t, MatView x, CkptView out, int64_t rows, int64_t cols,
                              hipStream_t stream);
 hipError_t launch_restore(Elem t, CkptView c, MatView out, int64_t rows, int64_t cols,
@@ -74,6 +77,9 @@ struct GroupArgs {
 hipError_t launch_grouped_product(Elem t, const GroupArgs& g, hipStream_t stream);
 hipError_t launch_grouped_input_grad(Elem t, const GroupArgs& g, hipStream_t stream);
 hipError_t launch_grouped_weight_grad(Elem t, const GroupArgs& g, hipStream_t stream);
+// Whether some tile covers a product of these sizes within kMaxWorkgroups.
+bool row_product_fits(int64_t rows, int64_t experts, int64_t width);
+bool weight_grad_fits(int64_t experts, int64_t n, int64_t k);
 // Partial sums (n x k fp32 each) that the weight gradient of these sizes needs
 // room for: long experts are cut into parts where whole ones would leave CUs idle.
 int64_t weight_grad_partials(int64_t rows, int64_t experts, int64_t n, int64_t k, int cus);

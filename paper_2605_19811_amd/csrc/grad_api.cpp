@@ -25,7 +25,6 @@ static_assert(LM_CHECKPOINT_BLOCK == lm::kCkptBlock, "one block length");
 
 constexpr int64_t kMaxLd = int64_t(1) << 22;      // elements between rows
 constexpr int64_t kMaxRows = (int64_t(1) << 31) - 1;
-constexpr int64_t kMaxGrid = (int64_t(1) << 31) - 1;
 
 // A rejected argument; the entry points turn it into a status.
 struct Bad {
@@ -188,9 +187,8 @@ void check_group(const lm_stack* w, const int32_t* offsets, int64_t rows) {
 void need_half(const char* name, int32_t dtype) {
   if (dtype == LM_F32) throw Bad{LM_ERR_UNSUPPORTED, std::string(name) + ": products take bf16 or fp16"};
 }
-// Smallest tiles that any variant uses: no grid is larger.
-void check_grid(int64_t a, int64_t b, int64_t c) {
-  if (double(a) * double(b) * double(c) > double(kMaxGrid)) throw Bad{LM_ERR_UNSUPPORTED, "too many tiles for one launch"};
+void check_grid(bool fits) {
+  if (!fits) throw Bad{LM_ERR_UNSUPPORTED, "too many tiles for one launch"};
 }
 
 size_t partial_bytes(int64_t rows, int64_t count, int64_t n, int64_t k) {
@@ -390,7 +388,7 @@ lm_status lionmuon_grouped_product(const lm_matrix* x, const lm_stack* w, const 
     same_shape("y", y, x->rows, w->rows);
     need_half("x", x->dtype);
     need(w->dtype == x->dtype && y->dtype == x->dtype, "x, w and y must have one type");
-    check_grid(x->rows / 16 + w->count, w->rows / 64 + 1, 1);
+    check_grid(lm::row_product_fits(x->rows, w->count, w->rows));
     apart({span("y", y)}, {span("x", x), span("w", w), span("offsets", offsets, 1, 0, (w->count + 1) * 4)});
     if (x->rows == 0) return hipSuccess;
     GroupArgs g;
@@ -423,7 +421,7 @@ lm_status lionmuon_grouped_input_grad(const lm_matrix* dy, const lm_stack* w,
     same_shape("dx", dx, dy->rows, w->cols);
     need_half("dy", dy->dtype);
     need(w->dtype == dy->dtype && dx->dtype == dy->dtype, "dy, w and dx must have one type");
-    check_grid(dy->rows / 16 + w->count, w->cols / 64 + 1, 1);
+    check_grid(lm::row_product_fits(dy->rows, w->count, w->cols));
     apart({span("dx", dx)}, {span("dy", dy), span("w", w), span("offsets", offsets, 1, 0, (w->count + 1) * 4)});
     if (dy->rows == 0) return hipSuccess;
     GroupArgs g;
@@ -480,7 +478,7 @@ lm_status lionmuon_grouped_weight_grad(const lm_matrix* dy, const lm_matrix* x,
       if (dy->dtype != LM_BF16)
         throw Bad{LM_ERR_UNSUPPORTED, "dy must be bf16 with a checkpoint (fp16 does not hold its values)"};
     }
-    check_grid(dw->rows / 64 + 1, dw->cols / 64 + 1, dw->count);
+    check_grid(lm::weight_grad_fits(dw->count, dw->rows, dw->cols));
     const size_t wanted = partial_bytes(dy->rows, dw->count, dw->rows, dw->cols);
     check_workspace(workspace, workspace_bytes, wanted);
     apart({span("dw", dw), span("workspace", workspace, 1, 0, int64_t(wanted))},

@@ -4,19 +4,27 @@
 //   dX = dY W_e        W_e across it: n runs over its rows         (kRows, kCols)
 //   dW_e = dY_e^T X_e  both across it: the rows of an expert       (kCols, kCols)
 //
-// One tile kernel serves all three. The contraction goes through LDS 64 values
-// at a time, double buffered. An operand that runs along the contraction is
-// staged as rows of 64 values (128 bytes, eight 16-byte chunks XOR-swizzled by
-// row); one that runs across it as 64 rows of the tile's width, read through
-// gfx950's LDS transpose reads, so that no operand is ever transposed in memory.
+// One tile kernel serves all three. The contraction goes through LDS in stages of
+// 64 values. An operand that runs along the contraction is staged as rows of 64
+// values (128 bytes, eight 16-byte chunks XOR-swizzled by row); one that runs across
+// it as 64 rows of the tile's width, read through gfx950's LDS transpose reads, so
+// that no operand is ever transposed in memory. 256 x 256 tiles take 8192^3 at
+// 1330 TFLOP/s and 4096^3 at 1250 (the library's product: 1590, 1510): their 64 KB
+// of operands a stage, copied in 1 KB pieces, bound them (without copies 1340 -> 1470,
+// the matrix unit's own rate under the power limit). What it took, each
+// measured on the kernel before: all stages' fragments read a step ahead and one
+// barrier a stage (853 -> 1104 at 8192^3), tiles counted on the device (an XCD with
+// two tiles more than CUs made every product take a round more: 4096^3 200 -> 110 us),
+// eight waves a tile instead of four (16384 x 4096 x 1024: 960 -> 1030).
 //
 // The host knows the total of rows and the number of experts, never the rows of
 // each: the grid covers the most row tiles that any split into experts can need,
-// and a workgroup finds its expert and tile from the offsets (find_tile).
+// and a workgroup finds its expert and tile from the offsets (find_group).
 //
 // Ragged edges cost no branch in the loop: operands are read by buffer loads
 // whose descriptor ends at the last valid row, so what lies beyond reads as zero,
-// and lanes beyond the end of the contraction get an address outside.
+// and lanes beyond the end of the contraction get an address outside. Operands off
+// 16 bytes go through registers instead (4096^3 with rows of odd length: 147 us).
 #include <algorithm>
 #include <type_traits>
 
@@ -149,19 +157,26 @@ __device__ __forceinline__ int by_xcd(int bid, int chunk) {
   return (j / chunk * 8 + x) * chunk + j % chunk;
 }
 
-// The nth longest expert (n-th in order where there are too many to sort on
+// The nth longest expert (the nth in order where there are too many to sort on
 // the way): workgroups start in this order, so that no long one starts last.
+// Selected bit by bit from the top, of equal ones in order.
 __device__ __forceinline__ int nth_longest(const int32_t* offsets, int experts, int rows, int n) {
   if (experts == 1 || experts > 64) return n;
   const int lane = threadIdx.x & 63, i = min(lane, experts - 1);
-  const int len = lane < experts ? min(max(offsets[i + 1], 0), rows) - min(max(offsets[i], 0), rows) : INT32_MIN;
-  int rank = 0;
-  for (int j = 0; j < experts; ++j) {
-    const int other = __builtin_amdgcn_readlane(len, j);
-    rank += other > len || (other == len && j < lane) ? 1 : 0;
+  const int len = max(min(max(offsets[i + 1], 0), rows) - min(max(offsets[i], 0), rows), 0);
+  uint64_t left = experts == 64 ? ~0ull : (1ull << experts) - 1;
+  for (int bit = 31 - __builtin_clz(rows | 1); bit >= 0; --bit) {
+    const uint64_t m = __ballot((len >> bit) & 1) & left;
+    const int c = __builtin_popcountll(m);
+    if (n < c) {
+      left = m;
+    } else {
+      n -= c;
+      left &= ~m;
+    }
   }
-  const uint64_t m = __ballot(lane < experts && rank == n);
-  return __builtin_amdgcn_readfirstlane(63 - __builtin_clzll(m | 1));
+  for (; n > 0; --n) left &= left - 1;
+  return __builtin_amdgcn_readfirstlane(__builtin_ctzll(left | 1ull << 63));
 }
 
 // Tile `id` of m x n as (row, column), in bands of eight rows: the tiles that run
@@ -971,6 +986,15 @@ constexpr TileCost kWeightTiles[3] = {{256, 128, 1, 0.7, 1.0, 6.0}, {128, 128, 2
 
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
+// Workgroups of a row product's whole tiles: the most that any split of the rows
+// into experts makes.
+int64_t row_workgroups(const TileCost& c, int64_t rows, int64_t experts, int64_t width) {
+  return (rows / c.bm + std::min(experts, rows)) * ceil_div(width, c.bn) + 2048;
+}
+int64_t weight_workgroups(const TileCost& c, int64_t experts, int64_t n, int64_t k) {
+  return 2 * experts * ceil_div(n, c.bm) * ceil_div(k, c.bn) + 65536;     // (parts: at most a few tiles for each CU)
+}
+
 // Tile of a row product: the least time by rounds of tiles over the CUs, the last one
 // in quarters where the kernel does that. An expert's last tile is half empty on average.
 int row_tile(int64_t rows, int64_t experts, int64_t width, int64_t depth, int cus, bool aligned) {
@@ -985,7 +1009,7 @@ int row_tile(int64_t rows, int64_t experts, int64_t width, int64_t depth, int cu
     double t = double(tiles / places) * (c.full * stages + c.rest);
     if (i == 0 && aligned && left * 2 <= cus) t += left > 0 ? kRowTiles[1].alone * (left * 4 <= cus ? 1.0 : 1.5) * stages + c.rest : 0.0;
     else if (left > 0) t += (left <= cus && i > 0 ? c.alone : left * 4 <= cus ? c.alone : c.full) * stages + c.rest;
-    if (i == 0 || t < least) {
+    if (i == 0 || (t < least && row_workgroups(c, rows, experts, width) <= kMaxWorkgroups)) {
       best = i;
       least = t;
     }
@@ -1006,6 +1030,7 @@ WeightPlan weight_plan(int64_t rows, int64_t experts, int64_t n, int64_t k, int 
   double least = -1.0;
   for (int i = 0; i < 3; ++i) {
     const TileCost& c = kWeightTiles[i];
+    if (i > 0 && weight_workgroups(c, experts, n, k) > kMaxWorkgroups) break;
     const int64_t per = ceil_div(n, c.bm) * ceil_div(k, c.bn), tiles = experts * per, places = int64_t(cus) * c.at_once;
     const double share = double(rows) * double(per) / double(places);      // rows of each place
     const double longest = experts == 1 ? double(rows) : std::min(double(rows), 3.0 * double(rows) / double(experts));
@@ -1163,6 +1188,14 @@ hipError_t launch_grouped_weight_grad(Elem t, const GroupArgs& g, hipStream_t st
   else if (t == Elem::kBF16) weight_product<bf16, kCols>(g, stream);
   else weight_product<f16, kCols>(g, stream);
   return hipGetLastError();
+}
+
+bool row_product_fits(int64_t rows, int64_t experts, int64_t width) {
+  return row_workgroups(kRowTiles[0], rows, experts, width) <= kMaxWorkgroups;
+}
+
+bool weight_grad_fits(int64_t experts, int64_t n, int64_t k) {
+  return weight_workgroups(kWeightTiles[0], experts, n, k) <= kMaxWorkgroups;
 }
 
 int64_t weight_grad_partials(int64_t rows, int64_t experts, int64_t n, int64_t k, int cus) {

@@ -82,6 +82,9 @@ BlockWalk walk_of(int64_t rows, int64_t cols) {
   w.blocks = int32_t((cols + kCkptBlock - 1) / kCkptBlock);
   const int64_t want = rows * w.blocks >= 256 * 64 ? 64 : 16;
   w.per = int32_t(w.blocks >= want ? 1 : want / w.blocks);
+  // (a launch has fewer than 2^32 threads)
+  const int64_t least = (rows + kMaxWorkgroups - 1) / kMaxWorkgroups;
+  if (w.per < least) w.per = int32_t(least);
   return w;
 }
 

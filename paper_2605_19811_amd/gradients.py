@@ -110,7 +110,7 @@ class Checkpoint:
         ld_scales, step_scales = scales.stride()
         if (cols > 1 and step != 1) or (blocks > 1 and step_scales != 1):
             _invalid("the rows of codes and scales must be contiguous")
-        if ld_scales % 4 == 0 and rows * ld_scales > \
+        if rows > 1 and ld_scales % 4 == 0 and rows * ld_scales > \
                 scales.untyped_storage().nbytes() - scales.storage_offset():
             _invalid("the last row of scales must be as long as the others")
         self.shape = codes.shape

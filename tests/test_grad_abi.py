@@ -280,3 +280,21 @@ def test_binding_refuses_host_tensors_and_wrong_kinds():
         gr.Checkpoint(torch.zeros(4, 129, dtype=u8), torch.zeros(4, 1, dtype=u8))
     k = gr.Checkpoint.empty(3, 129, "cpu")
     assert k.shape == (3, 129) and k.codes.stride(0) == 144 and k.scales.shape == (3, 2)
+
+
+def test_products_too_large_for_a_launch_are_refused(lib):
+    w = stack(1, 1 << 20, 4096, 64)
+    refused(lib, lib.lionmuon_grouped_product(mat(0, 1 << 26, 64), w, at(2), mat(3, 1 << 26, 4096), None),
+            UNSUPPORTED, "tiles")
+    refused(lib, lib.lionmuon_grouped_weight_grad(mat(0, 8, 4096), mat(4, 8, 64), None, at(2),
+                                                  stack(1, 1 << 20, 4096, 64, dtype=F32), 0, None, 0, None),
+            UNSUPPORTED, "tiles")
+
+
+def test_checkpoint_with_a_short_last_row_of_scales_is_refused():
+    import torch
+    u8 = torch.uint8
+    scales = torch.as_strided(torch.zeros(7, dtype=u8), (2, 3), (4, 1))
+    with pytest.raises(lm.LionMuonError):
+        gr.Checkpoint(torch.zeros(2, 384, dtype=u8), scales)
+    gr.Checkpoint(torch.zeros(2, 384, dtype=u8), torch.as_strided(torch.zeros(8, dtype=u8), (2, 3), (4, 1)))
