@@ -9,13 +9,15 @@
 // values (128 bytes, eight 16-byte chunks XOR-swizzled by row); one that runs across
 // it as 64 rows of the tile's width, read through gfx950's LDS transpose reads, so
 // that no operand is ever transposed in memory. 256 x 256 tiles take 8192^3 at
-// 1330 TFLOP/s and 4096^3 at 1250 (the library's product: 1590, 1510): their 64 KB
+// 1340 TFLOP/s and 4096^3 at 1250 (the library's product: 1590, 1510): their 64 KB
 // of operands a stage, copied in 1 KB pieces, bound them (without copies 1340 -> 1470,
 // the matrix unit's own rate under the power limit). What it took, each
 // measured on the kernel before: all stages' fragments read a step ahead and one
 // barrier a stage (853 -> 1104 at 8192^3), tiles counted on the device (an XCD with
 // two tiles more than CUs made every product take a round more: 4096^3 200 -> 110 us),
-// eight waves a tile instead of four (16384 x 4096 x 1024: 960 -> 1030).
+// eight waves a tile instead of four (16384 x 4096 x 1024: 960 -> 1030), the next
+// tile's copies during a tile's last stages (the same by eight experts: 142 -> 132 us;
+// without stores it would be 119: they do not overlap with anything else).
 //
 // The host knows the total of rows and the number of experts, never the rows of
 // each: the grid covers the most row tiles that any split into experts can need,
@@ -101,49 +103,54 @@ __device__ __forceinline__ uint32_t lds_address(const void* p) {
 struct Span {
   int expert, index, row0, end;      // row0: of the expert's group `index`
 };
-__device__ __forceinline__ int groups_of(const int32_t* offsets, int experts, int rows, int bm, int least, int i, int* first, int* end) {
-  const int j = min(i, experts - 1);
-  *first = min(max(offsets[j], 0), rows);
-  *end = min(max(offsets[j + 1], 0), rows);
-  return i < experts ? max((max(*end - *first, 0) + bm - 1) / bm, least) : 0;
-}
-__device__ __forceinline__ int wave_scan(int v, int lane) {      // inclusive
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const int up = __shfl_up(v, d, 64);
-    v += lane >= d ? up : 0;
-  }
+struct Groups {
+  int first, end, upto;              // of the lane's expert: its rows, groups up to and with its own
+};
+// By lane shifts within 16 lanes, then the sums of the 16 and 32 lanes below.
+__device__ __forceinline__ int wave_scan(int v) {      // inclusive
+  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, false);   // row_shr:1
+  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false);   // row_bcast:15
+  v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);   // row_bcast:31
   return v;
 }
-__device__ __forceinline__ int count_groups(const int32_t* offsets, int experts, int rows, int bm, int least) {
-  const int lane = threadIdx.x & 63;
+__device__ __forceinline__ Groups groups_from(const int32_t* offsets, int experts, int rows, int bm, int least, int base) {
+  const int i = base + int(threadIdx.x & 63), j = min(i, experts - 1);
+  Groups g;
+  g.first = min(max(offsets[j], 0), rows);
+  g.end = min(max(offsets[j + 1], 0), rows);
+  g.upto = wave_scan(i < experts ? max((max(g.end - g.first, 0) + bm - 1) / bm, least) : 0);
+  return g;
+}
+// All groups; *last: the last 64 experts', all of them where there are no more.
+__device__ __forceinline__ int count_groups(const int32_t* offsets, int experts, int rows, int bm, int least, Groups* last) {
   int total = 0;
   for (int base = 0; base < experts; base += 64) {
-    int first, end;
-    const int n = groups_of(offsets, experts, rows, bm, least, base + lane, &first, &end);
-    total += __builtin_amdgcn_readlane(wave_scan(n, lane), 63);
+    *last = groups_from(offsets, experts, rows, bm, least, base);
+    total += __builtin_amdgcn_readlane(last->upto, 63);
   }
   return total;
 }
+__device__ __forceinline__ Span group_of(const Groups& g, int base, int bm, int id) {
+  const int l = __builtin_ctzll(__ballot(g.upto > id) | 1ull << 63);
+  Span t;
+  t.expert = base + l;
+  t.index = id - (l > 0 ? __builtin_amdgcn_readlane(g.upto, max(l - 1, 0)) : 0);
+  t.row0 = __builtin_amdgcn_readlane(g.first, l) + t.index * bm;
+  t.end = __builtin_amdgcn_readlane(g.end, l);
+  return t;
+}
 // Group `id` (below the count).
-__device__ __forceinline__ Span find_group(const int32_t* offsets, int experts, int rows, int bm, int least, int id) {
-  const int lane = threadIdx.x & 63;
-  Span t{0, 0, 0, 0};
-  for (int base = 0; base < experts; base += 64) {
-    int first, end;
-    const int n = groups_of(offsets, experts, rows, bm, least, base + lane, &first, &end);
-    const int upto = wave_scan(n, lane), here = __builtin_amdgcn_readlane(upto, 63);
-    if (id < here) {
-      const int l = __builtin_ctzll(__ballot(upto > id));
-      t.expert = base + l;
-      t.index = id - (__builtin_amdgcn_readlane(upto, l) - __builtin_amdgcn_readlane(n, l));
-      t.row0 = __builtin_amdgcn_readlane(first, l) + t.index * bm;
-      t.end = __builtin_amdgcn_readlane(end, l);
-      break;
-    }
+__device__ __forceinline__ Span find_group(const int32_t* offsets, int experts, int rows, int bm, int least, int id, const Groups& last) {
+  if (experts <= 64) return group_of(last, 0, bm, id);
+  for (int base = 0;; base += 64) {
+    const Groups g = groups_from(offsets, experts, rows, bm, least, base);
+    const int here = __builtin_amdgcn_readlane(g.upto, 63);
+    if (id < here || base + 64 >= experts) return group_of(g, base, bm, id);
     id -= here;
   }
-  return t;
 }
 
 enum { kRows = 0, kCols = 1, kCodes = 2 };   // operand: along, across, across in 8 bits
@@ -664,6 +671,97 @@ struct Tile {
     }
     wait_vmcnt<0>();
   }
+
+  // The products of several tiles, one after the other, as one run of stages: the
+  // last two of a tile are followed by the copies of the next one's first two, so
+  // that no tile but the first waits for its operands. next(a, b) points the sources
+  // at the next tile (or at nothing); done(out) writes the tile that is complete, in LDS
+  // behind the stages, and says whether another one follows.
+  template <class Next, class Done>
+  __device__ static __forceinline__ void products(const Source& a, const Source& b, int depth, char* smem, Next next, Done done) {
+    static_assert(DA && DB && MB != kCodes && NB == 2 && KS / 16 / SUB == 2, "two stages of two steps");
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wm = (wave / kWavesN) * WM, wn = (wave % kWavesN) * WN;
+    const int nk = max((depth + KS - 1) / KS, 2);      // (a second stage may lie past the end: zeros)
+    constexpr int kCopiesA = Copier<MA, BM>::kInst, kCopies = kCopiesA + Copier<MB, BN>::kInst;
+    Copier<MA, BM> ca(a, wave, lane);
+    Copier<MB, BN> cb(b, wave, lane);
+    auto start = [&](int kt) {
+      ca.start(kt * KS);
+      cb.start(kt * KS);
+    };
+    const uint32_t lds = lds_address(smem) + wave * 1024;
+    auto copy = [&](int q, int buf) {
+      if (q < kCopiesA) ca.copy(q, lds + buf);
+      else cb.copy(q - kCopiesA, lds + buf + kStageA);
+    };
+#pragma unroll
+    for (int kt = 0; kt < 2; ++kt) {
+      start(kt);
+#pragma unroll
+      for (int q = 0; q < kCopies; ++q) copy(q, kt * kStageBytes);
+    }
+    wait_vmcnt<kCopies>();
+    lds_barrier();
+    constexpr int kFrags = SUB * (kMI + kNI), kMfmas = SUB * kMI * kNI;
+    s16x8 fa[2][SUB * kMI], fb[2][SUB * kNI];
+    auto read = [&](int slot, int buf, int st, int f) {
+      const int u = f / (kMI + kNI), g = f % (kMI + kNI);
+      const char* p = smem + buf;
+      if (g < kMI) fa[slot][u * kMI + g] = fragment<MA, BM>(p, wm + 32 * g, st * SUB + u, lane);
+      else fb[slot][u * kNI + g - kMI] = fragment<MB, BN>(p + kStageA, wn + 32 * (g - kMI), st * SUB + u, lane);
+    };
+#pragma unroll
+    for (int f = 0; f < kFrags; ++f) read(0, 0, 0, f);
+    f32x16 out[kMI][kNI];
+    // step `st` of a stage, whose fragments are in slot `st` (see product)
+    auto step = [&](int st, int buf1, int fill) {
+#pragma unroll
+      for (int m = 0; m < kMfmas; ++m) {
+        const int u = m / (kMI * kNI), i = m / kNI % kMI, j = m % kNI;
+        out[i][j] = mma(fb[st][u * kNI + j], fa[st][u * kMI + i], out[i][j], T());
+#pragma unroll
+        for (int f = m * kFrags / kMfmas; f < (m + 1) * kFrags / kMfmas; ++f) read(st ^ 1, buf1, st ^ 1, f);
+        if (st == 1) {
+#pragma unroll
+          for (int q = m * kCopies / kMfmas; q < (m + 1) * kCopies / kMfmas; ++q) copy(q, fill);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    };
+    int buf = 0;
+    bool landed = false;                               // the second stage of a tile, before its first
+    for (;;) {
+#pragma unroll
+      for (int i = 0; i < kMI; ++i)
+#pragma unroll
+        for (int j = 0; j < kNI; ++j) out[i][j] = f32x16(0.0f);
+      // the stages that copy this tile's, then the two that copy the next one's
+#pragma unroll 1
+      for (int part = 0; part < 2; ++part) {
+        if (part == 1) next(ca.s, cb.s);
+        const int n = part == 0 ? nk : 2;
+#pragma unroll 1
+        for (int kt = part == 0 ? 2 : 0; kt < n; ++kt) {
+          step(0, buf, 0);
+          // (of the wave's copies none but the next stage's are in flight)
+          if (!landed) wait_vmcnt<0>();
+          landed = false;
+          lds_barrier();
+          start(kt);
+          __builtin_amdgcn_sched_barrier(0);
+          step(1, kStageBytes - buf, buf);
+          __builtin_amdgcn_sched_barrier(0);
+          buf = kStageBytes - buf;
+        }
+      }
+      // waited for here: after the stores of `done` a wait would include them
+      wait_vmcnt<0>();
+      landed = true;
+      if (!done(out)) return;
+    }
+  }
 };
 
 // ---------------------------------------------------------------------------
@@ -678,41 +776,42 @@ struct RowProduct {
   int rows, experts;
   int width, depth;                   // columns of the output, contraction
   int tiles_n;
-  int places, main;                   // CUs, workgroups for whole tiles
+  int places, main;                   // large tiles: CUs, workgroups for whole tiles
 };
 
-// One tile: rows row0 .. of expert `e`, whose rows end at `end`, columns from col0 on.
-template <typename T, class K>
-__device__ __forceinline__ void row_product_tile(const RowProduct& g, char* smem, int expert, int row0, int end, int col0) {
-  constexpr int BM = K::BM, BN = K::BN, WM = K::WM, WN = K::WN, MB = K::kModeOfB;
-  constexpr int kStage = 32 * (WN + 8);         // elements of a wave's output staging
-  static_assert(K::kWaves * kStage * 2 <= K::kLds, "staging fits");
+// Operands of a tile: rows row0 .. of expert `expert`, whose rows end at `end`, and
+// columns from col0 on.
+template <typename T, int MB, class K>
+__device__ __forceinline__ void row_product_sources(const RowProduct& g, int expert, int row0, int end, int col0, Source* a, Source* b) {
   const T* w = static_cast<const T*>(g.b) + expert * g.b_stride;
-  Source a, b;
-  a.p = reinterpret_cast<const char*>(static_cast<const T*>(g.a) + row0 * g.lda);
-  a.ld = g.lda * 2;
-  a.rows = min(end - row0, BM);
-  a.depth = g.depth;
-  a.cols = 0;
-  a.wide = g.depth >= 8;
-  b.p = reinterpret_cast<const char*>(MB == kRows ? w + col0 * g.ldb : w + col0);
-  b.ld = g.ldb * 2;
-  b.rows = min(g.width - col0, BN);
-  b.cols = g.width - col0;
-  b.depth = g.depth;
-  b.wide = (MB == kRows ? g.depth : g.width) >= 8;
-  f32x16 acc[K::kMI][K::kNI];
-  K::template product<0>(a, b, typename K::CodeSource{}, g.depth, smem, acc);
-  lds_barrier();
-  // Output through LDS, 32 rows of a wave at a time: rows of 16-bit values
-  // leave as whole 16-byte pieces. Element r of a block is row lane % 32, column
-  // 8 (r / 4) + 4 (lane / 32) + r % 4 (B is the matrix unit's first operand, so
-  // that a lane has four columns in a row: an LDS write each).
+  a->p = reinterpret_cast<const char*>(static_cast<const T*>(g.a) + row0 * g.lda);
+  a->ld = g.lda * 2;
+  a->rows = min(end - row0, K::BM);
+  a->depth = g.depth;
+  a->cols = 0;
+  a->wide = g.depth >= 8;
+  b->p = reinterpret_cast<const char*>(MB == kRows ? w + col0 * g.ldb : w + col0);
+  b->ld = g.ldb * 2;
+  b->rows = min(g.width - col0, K::BN);
+  b->cols = g.width - col0;
+  b->depth = g.depth;
+  b->wide = (MB == kRows ? g.depth : g.width) >= 8;
+}
+
+// Writes a tile through LDS, 32 rows of a wave at a time, so that rows of 16-bit
+// values leave as whole 16-byte pieces. Element r of a block is row lane % 32, column
+// 8 (r / 4) + 4 (lane / 32) + r % 4 (B is the matrix unit's first operand, so
+// that a lane has four columns in a row: an LDS write each). Pieces are
+// XOR-swizzled by row: eight rows of one piece fall into different banks.
+template <typename T, class K>
+__device__ __forceinline__ void write_row_product(const RowProduct& g, char* smem, int row0, int end, int col0, const f32x16 (&acc)[K::kMI][K::kNI]) {
+  constexpr int WM = K::WM, WN = K::WN, kPer = WN / 8;
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wm = (wave / K::kWavesN) * WM, wn = (wave % K::kWavesN) * WN;
-  T* st = reinterpret_cast<T*>(smem) + wave * kStage;
+  T* st = reinterpret_cast<T*>(smem) + wave * 32 * WN;
   T* out = static_cast<T*>(g.c);
+  auto piece = [](int r, int c) { return r * WN + ((c ^ (r * kPer / 8)) & (kPer - 1)) * 8; };
 #pragma unroll
   for (int i = 0; i < K::kMI; ++i) {
 #pragma unroll
@@ -724,17 +823,17 @@ __device__ __forceinline__ void row_product_tile(const RowProduct& g, char* smem
         for (int x = 0; x < 4; ++x) v[x] = T(acc[i][j][4 * r + x]);
         u32x2 u;
         __builtin_memcpy(&u, v, 8);
-        *reinterpret_cast<u32x2*>(st + (lane & 31) * (WN + 8) + 32 * j + 8 * r + 4 * (lane >> 5)) = u;
+        *reinterpret_cast<u32x2*>(st + piece(lane & 31, 4 * j + r) + 4 * (lane >> 5)) = u;
       }
     // (a wave's own region: its LDS accesses are in order)
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    constexpr int kPer = WN / 8;
 #pragma unroll
     for (int q = 0; q < 32 * kPer / 64; ++q) {
-      const int r = (q * 64 + lane) / kPer, c = (lane % kPer) * 8;
-      const int row = row0 + wm + 32 * i + r, col = col0 + wn + c;
+      const int r = (q * 64 + lane) / kPer, c = lane % kPer;
+      const int row = row0 + wm + 32 * i + r, col = col0 + wn + c * 8;
       if (row >= end || col >= g.width) continue;
-      const u32x4 v = *reinterpret_cast<const u32x4*>(st + r * (WN + 8) + c);
+      const T* from = st + piece(r, c);
+      const u32x4 v = *reinterpret_cast<const u32x4*>(from);
       T* p = out + int64_t(row) * g.ldc + col;
       if (col + 8 <= g.width) {
         // (tiles of 64 columns a wave and more write whole lines)
@@ -743,46 +842,96 @@ __device__ __forceinline__ void row_product_tile(const RowProduct& g, char* smem
       } else {
 #pragma unroll
         for (int e = 0; e < 8; ++e)
-          if (col + e < g.width) p[e] = st[r * (WN + 8) + c + e];
+          if (col + e < g.width) p[e] = from[e];
       }
     }
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
   }
 }
 
-// Q: quarters of S's tile. Tiles that would be a last round on at most half the CUs run as
-// four of them each, two to a CU if need be, in workgroups behind the others
-// (4096 x 1024 by 16384 rows: 16 of 272 tiles).
-template <typename T, int MB, class S, class Q, bool DA, bool DB>
+template <typename T, class K>
+__device__ __forceinline__ void row_product_tile(const RowProduct& g, char* smem, int expert, int row0, int end, int col0) {
+  static_assert(K::kWaves * 32 * K::WN * 2 <= K::kLds, "staging fits");
+  Source a, b;
+  row_product_sources<T, K::kModeOfB, K>(g, expert, row0, end, col0, &a, &b);
+  f32x16 acc[K::kMI][K::kNI];
+  K::template product<0>(a, b, typename K::CodeSource{}, g.depth, smem, acc);
+  lds_barrier();
+  write_row_product<T, K>(g, smem, row0, end, col0, acc);
+}
+
+// A tile a workgroup.
+template <typename T, int MB, class S, bool DA, bool DB>
 __global__ __launch_bounds__(S::kThreads, S::kWorkgroups) void row_product_kernel(RowProduct g) {
   using K = Tile<T, kRows, MB, S, DA, DB>;
-  constexpr int BM = S::BM, BN = S::BN;
-  constexpr bool kTail = !std::is_void_v<Q>;
   __shared__ __align__(16) char smem[K::kLds];
   // An XCD (every eighth workgroup) takes an eighth of the tiles that there
   // are, neighbours that share operands in its L2.
-  const int tiles_m = count_groups(g.offsets, g.experts, g.rows, BM, 0), tiles = tiles_m * g.tiles_n;
-  const int rest = kTail ? tiles % g.places : 0, tail = 2 * rest <= g.places ? rest : 0;
-  const bool behind = kTail && int(blockIdx.x) >= g.main;
-  const int number = behind ? blockIdx.x - g.main : blockIdx.x, turn = number / 8 / (behind ? 4 : 1);
-  const int count = behind ? tail : tiles - tail, each = (count + 7) / 8;
-  int id = number % 8 * each + turn;
-  if (turn >= each || id >= count) return;
-  if (behind) id += tiles - tail;
+  Groups groups;
+  const int tiles_m = count_groups(g.offsets, g.experts, g.rows, S::BM, 0, &groups), tiles = tiles_m * g.tiles_n;
+  const int turn = blockIdx.x / 8, each = (tiles + 7) / 8, id = blockIdx.x % 8 * each + turn;
+  if (turn >= each || id >= tiles) return;
   int tm, tn;
   banded(id, tiles_m, g.tiles_n, &tm, &tn);
-  const Span t = find_group(g.offsets, g.experts, g.rows, BM, 0, tm);
-  if constexpr (kTail) {
-    if (behind) {
-      static_assert(Q::BM * 2 == BM && Q::BN * 2 == BN && Q::kThreads == S::kThreads, "quarters");
-      using KQ = Tile<T, kRows, MB, Q, DA, DB>;
-      static_assert(KQ::kLds <= K::kLds, "one block of LDS");
-      const int q = number / 8 % 4, row0 = t.row0 + (q >> 1) * Q::BM, col0 = tn * BN + (q & 1) * Q::BN;
-      if (row0 < t.end && col0 < g.width) row_product_tile<T, KQ>(g, smem, t.expert, row0, t.end, col0);
-      return;
-    }
+  const Span t = find_group(g.offsets, g.experts, g.rows, S::BM, 0, tm, groups);
+  row_product_tile<T, K>(g, smem, t.expert, t.row0, t.end, tn * S::BN);
+}
+
+// Large tiles: g.main workgroups, one for each CU, take every (g.main / 8)th tile of their
+// XCD's eighth, in the order in which single ones would start. Q: quarters of S's
+// tile. Tiles that would be a last round on at most half the CUs run as four of
+// them each, two to a CU if need be, in workgroups behind the others (4096 x 1024
+// by 16384 rows: 16 of 272 tiles).
+template <typename T, int MB, class S, class Q>
+__global__ __launch_bounds__(S::kThreads, 1) void row_products_kernel(RowProduct g) {
+  using K = Tile<T, kRows, MB, S, true, true>;
+  using KQ = Tile<T, kRows, MB, Q, true, true>;
+  constexpr int BM = S::BM, BN = S::BN;
+  static_assert(Q::BM * 2 == BM && Q::BN * 2 == BN && Q::kThreads == S::kThreads, "quarters");
+  static_assert(KQ::kLds <= K::kLds, "one block of LDS");
+  __shared__ __align__(16) char smem[K::kLds + K::kWaves * 32 * S::WN * 2];
+  Groups groups;
+  const int tiles_m = count_groups(g.offsets, g.experts, g.rows, BM, 0, &groups), tiles = tiles_m * g.tiles_n;
+  const int rest = tiles % g.places, tail = 2 * rest <= g.places ? rest : 0;
+  const bool behind = int(blockIdx.x) >= g.main;
+  const int number = behind ? blockIdx.x - g.main : blockIdx.x;
+  const int count = behind ? tail : tiles - tail, each = (count + 7) / 8, first = number % 8 * each;
+  int turn = number / 8 / (behind ? 4 : 1), tm, tn;
+  auto left = [&] { return turn < each && first + turn < count; };
+  if (!left()) return;
+  banded(first + turn + (behind ? tiles - tail : 0), tiles_m, g.tiles_n, &tm, &tn);
+  Span t = find_group(g.offsets, g.experts, g.rows, BM, 0, tm, groups);
+  if (behind) {
+    const int q = number / 8 % 4, row0 = t.row0 + (q >> 1) * Q::BM, col0 = tn * BN + (q & 1) * Q::BN;
+    if (row0 < t.end && col0 < g.width) row_product_tile<T, KQ>(g, smem, t.expert, row0, t.end, col0);
+    return;
   }
-  row_product_tile<T, K>(g, smem, t.expert, t.row0, t.end, tn * BN);
+  struct Place {
+    int row0, end, col0;
+  } here{t.row0, t.end, tn * BN}, then{0, 0, 0};
+  bool more = false;
+  Source a, b;
+  row_product_sources<T, MB, K>(g, t.expert, t.row0, t.end, tn * BN, &a, &b);
+  K::products(a, b, g.depth, smem,
+              [&](Source& sa, Source& sb) {
+                turn += g.main / 8;
+                more = left();
+                if (more) {
+                  banded(first + turn, tiles_m, g.tiles_n, &tm, &tn);
+                  // (scanned again: the registers are worth more)
+                  const Groups again = groups_from(g.offsets, g.experts, g.rows, BM, 0, 0);
+                  t = find_group(g.offsets, g.experts, g.rows, BM, 0, tm, again);
+                  then = Place{t.row0, t.end, tn * BN};
+                  row_product_sources<T, MB, K>(g, t.expert, t.row0, t.end, tn * BN, &sa, &sb);
+                } else {
+                  sa.rows = sb.rows = sa.depth = sb.depth = 0;
+                }
+              },
+              [&](const f32x16 (&acc)[K::kMI][K::kNI]) {
+                write_row_product<T, K>(g, smem + K::kLds, here.row0, here.end, here.col0, acc);
+                here = then;
+                return more;
+              });
 }
 
 // ---------------------------------------------------------------------------
@@ -827,8 +976,9 @@ __global__ __launch_bounds__(S::kThreads, S::kWorkgroups) void weight_product_ke
     t.row0 = min(max(g.offsets[t.expert], 0), g.rows);
     t.end = min(max(g.offsets[t.expert + 1], 0), g.rows);
   } else {
-    if (unit >= count_groups(g.offsets, g.experts, g.rows, g.part, 1)) return;
-    t = find_group(g.offsets, g.experts, g.rows, g.part, 1, unit);
+    Groups groups;
+    if (unit >= count_groups(g.offsets, g.experts, g.rows, g.part, 1, &groups)) return;
+    t = find_group(g.offsets, g.experts, g.rows, g.part, 1, unit, groups);
   }
   const int e = t.expert, i = t.index;
   const int row0 = __builtin_amdgcn_readfirstlane(t.row0);
@@ -1061,25 +1211,30 @@ template <typename T, int MB, class S, class Q, class R>
 void run_rows(RowProduct g, bool da, bool db, hipStream_t stream) {
   g.tiles_n = (g.width + S::BN - 1) / S::BN;
   // the most tiles that any split of the rows into experts makes
-  const int64_t tiles = (int64_t(g.rows) / S::BM + std::min(g.experts, g.rows)) * g.tiles_n;
-  g.main = int((tiles + 7) / 8 * 8);
+  const int64_t tiles = (int64_t(g.rows) / S::BM + std::min(g.experts, g.rows)) * g.tiles_n, whole = (tiles + 7) / 8 * 8;
   if (da && db) {
-    const int64_t quarters = std::is_void_v<Q> ? 0 : (std::min<int64_t>(tiles, g.places / 2) + 7) / 8 * 32;
-    row_product_kernel<T, MB, S, Q, true, true><<<dim3(unsigned(g.main + quarters)), S::kThreads, 0, stream>>>(g);
+    if constexpr (std::is_void_v<Q>) {
+      row_product_kernel<T, MB, S, true, true><<<dim3(unsigned(whole)), S::kThreads, 0, stream>>>(g);
+    } else {
+      g.places = std::max(g.places / 8 * 8, 8);
+      g.main = int(std::min<int64_t>(whole, g.places));
+      const int64_t quarters = (std::min<int64_t>(tiles, g.places / 2) + 7) / 8 * 32;
+      row_products_kernel<T, MB, S, Q><<<dim3(unsigned(g.main + quarters)), S::kThreads, 0, stream>>>(g);
+    }
     return;
   }
-  const dim3 grid(unsigned(g.main));
+  const dim3 grid{unsigned(whole)};
   if constexpr (MB == kCols) {       // (rows of Y = X W^T's operands are alike)
     if (db) {
-      row_product_kernel<T, MB, R, void, false, true><<<grid, R::kThreads, 0, stream>>>(g);
+      row_product_kernel<T, MB, R, false, true><<<grid, R::kThreads, 0, stream>>>(g);
       return;
     }
     if (da) {
-      row_product_kernel<T, MB, R, void, true, false><<<grid, R::kThreads, 0, stream>>>(g);
+      row_product_kernel<T, MB, R, true, false><<<grid, R::kThreads, 0, stream>>>(g);
       return;
     }
   }
-  row_product_kernel<T, MB, R, void, false, false><<<grid, R::kThreads, 0, stream>>>(g);
+  row_product_kernel<T, MB, R, false, false><<<grid, R::kThreads, 0, stream>>>(g);
 }
 
 template <typename T, int MB>

@@ -573,6 +573,27 @@ def test_large_products(experts, rows, n, k, pad):
         assert (out[int(at[-1]):] == 7.0).all()
 
 
+# several large tiles a workgroup, one after the other: contractions of less than a
+# stage, of one, two and a part of one; more experts than lanes, empty ones among them
+@pytest.mark.parametrize("experts,rows,n,k", [(1, 16400, 4104, 8), (1, 16400, 4104, 64), (3, 20000, 4096, 128),
+                                              (70, 30000, 2048, 136), (9, 40000, 2304, 200)])
+def test_products_of_several_rounds(experts, rows, n, k):
+    dt = torch.bfloat16
+    x, dy, w, offsets, at = group(rows, experts, n, k, dt, 53, lead=2, tail=3)
+    inside = slice(int(at[0]), int(at[-1]))
+    for call, a, b, depth, transpose in (
+            (gr.lionmuon_grouped_product, x, w, k, False),
+            (gr.lionmuon_grouped_input_grad, x, w.transpose(1, 2).contiguous(), k, True)):
+        want = gpu_products(call, a, b, at, transpose)
+        out = torch.full(want.shape, 7.0, dtype=dt, device="cuda")
+        call(a, b, offsets, out=out)
+        v = float(a[inside].double().square().mean() * b.double().square().mean()) ** 0.5
+        err = (out[inside].double() - want[inside]).abs()
+        assert (err <= half_step(dt) * 1.01 * want[inside].abs() + sum_bound(depth) * depth * v).all()
+        assert (out[:int(at[0])] == 7.0).all() and (out[int(at[-1]):] == 7.0).all()
+        assert torch.equal(call(a, b, offsets, out=torch.full_like(out, 7.0)), out)
+
+
 @pytest.mark.parametrize("experts,rows,n,k", [(1, 5000, 512, 1280), (3, 9000, 700, 640), (2, 700, 2560, 1152),
                                               (1, 70, 256, 128), (1, 20000, 300, 1000)])
 def test_weight_gradient_from_a_checkpoint_is_that_of_its_values(experts, rows, n, k):
