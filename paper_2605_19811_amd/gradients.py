@@ -186,7 +186,8 @@ def _matrix(t, name, device):
 
 def _new(rows, cols, like, code):
     """A new contiguous matrix of like's type and its descriptor."""
-    t = torch.empty((rows, cols), dtype=like.dtype, device=like.device)
+    t = torch.empty_like(like) if like.shape == (rows, cols) and like.is_contiguous() else \
+        like.new_empty((rows, cols))
     return t, lm_matrix(t.data_ptr(), rows, cols, cols, code, 0)
 
 
@@ -405,7 +406,7 @@ def lionmuon_rmsnorm(x, weight, residual=None, eps=1e-5, out=None, sum_out=None,
         y = my = None
     else:
         y, my = out, _matrix(out, "out", device)
-    rstd = torch.empty(rows, dtype=torch.float32, device=device)
+    rstd = weight.new_empty(rows)
     kept = _wanted(checkpoint, rows, cols, device)
     _done(_lib().lionmuon_rmsnorm(m, mr, w, eps, my, ms, rstd.data_ptr(),
                                   None if kept is None else kept._desc, handle),
@@ -448,7 +449,7 @@ def lionmuon_rmsnorm_grad(dy, s, weight, rstd, residual_grad=None, out=None, wei
     nbytes = 0
     if weight_grad is not False:
         if weight_grad is None:
-            dw = torch.empty(cols, dtype=torch.float32, device=device)
+            dw = torch.empty_like(weight)
             pw = dw.data_ptr()
         else:
             dw, pw = weight_grad, _vector(weight_grad, cols, "weight_grad", device)
