@@ -29,10 +29,10 @@
  *
  * Conventions shared by these entry points:
  *  - Descriptors (lm_matrix, lm_stack, lm_checkpoint) live in HOST memory, the
- *    pointers that they hold are DEVICE pointers. Rows may be apart (ld >= cols,
- *    in elements, below 2^22); the elements of a row are contiguous. Addresses need
- *    the element's alignment only; products run fastest where rows start
- *    16-byte aligned.
+ *    pointers that they hold are DEVICE pointers. At most 2^31 - 1 rows, which may
+ *    be apart (ld >= cols, in elements, below 2^22); the elements of a row are
+ *    contiguous. Addresses need the element's alignment only; products run
+ *    fastest where rows start 16-byte aligned.
  *  - Every call is asynchronous on `stream` (0 = the null stream), allocates
  *    nothing, keeps nothing from call to call and may be captured in a
  *    graph. Calls may run at the same time on different streams if their
@@ -121,7 +121,8 @@ lm_status lionmuon_activation_grad(const lm_matrix* dh, const lm_matrix* a,
  * Outputs, each may be NULL: y; sum = s (needs residual; may be the residual
  * itself: same data and ld); rstd (fp32, one a row, contiguous); kept =
  * checkpoint of y, rounded from fp32 once. weight: cols fp32 values. All
- * matrices have one type. cols in [1, LM_RMSNORM_MAX_COLS], eps >= 0.
+ * matrices have one type. cols in [1, LM_RMSNORM_MAX_COLS], eps >= 0. The mean is
+ * formed in fp32: where a row's sum of squares exceeds its range, rstd is 0.
  */
 lm_status lionmuon_rmsnorm(const lm_matrix* x, const lm_matrix* residual, const float* weight,
                            double eps, const lm_matrix* y, const lm_matrix* sum, float* rstd,
@@ -152,8 +153,11 @@ lm_status lionmuon_rmsnorm_workspace_bytes(int64_t rows, int64_t cols, size_t* o
  * offsets[0] .. offsets[count) belong to no expert: their inputs are not
  * used and their outputs left as they were. The host never reads offsets; offsets
  * that break the rule give unspecified values inside the outputs, nothing else.
- * X, dY, Y, dX and W: bf16 or fp16, one type. All columns counts >= 1.
+ * X, dY, Y, dX and W: bf16 or fp16, one type. All columns counts >= 1. Fewer than
+ * 2^30 rows, at most LM_GROUPED_MAX_EXPERTS experts (each workgroup goes through
+ * the offsets, 64 at a time).
  */
+#define LM_GROUPED_MAX_EXPERTS 65536
 
 /* Y[r] = X[r] W_e^T for each row r of expert e: x T x k, w count x n x k, y T x n. */
 lm_status lionmuon_grouped_product(const lm_matrix* x, const lm_stack* w, const int32_t* offsets,

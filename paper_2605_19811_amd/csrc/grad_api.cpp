@@ -25,6 +25,7 @@ static_assert(LM_CHECKPOINT_BLOCK == lm::kCkptBlock, "one block length");
 
 constexpr int64_t kMaxLd = int64_t(1) << 22;      // elements between rows
 constexpr int64_t kMaxRows = (int64_t(1) << 31) - 1;
+constexpr int64_t kMaxGroupedRows = int64_t(1) << 30;   // of a product: rows of a tile past it still fit an int
 
 // A rejected argument; the entry points turn it into a status.
 struct Bad {
@@ -181,8 +182,8 @@ void check_group(const lm_stack* w, const int32_t* offsets, int64_t rows) {
   need(w->rows >= 1 && w->cols >= 1, "n and k must be at least 1");
   need(w->count >= 1, "there must be at least one expert");
   need(offsets != nullptr && reinterpret_cast<uintptr_t>(offsets) % 4 == 0, "offsets: null or misaligned");
-  need(w->count <= (int64_t(1) << 20), "too many experts");
-  need(rows < (int64_t(1) << 30), "too many rows");
+  if (w->count > LM_GROUPED_MAX_EXPERTS) throw Bad{LM_ERR_UNSUPPORTED, "too many experts"};
+  need(rows < kMaxGroupedRows, "too many rows");
 }
 void need_half(const char* name, int32_t dtype) {
   if (dtype == LM_F32) throw Bad{LM_ERR_UNSUPPORTED, std::string(name) + ": products take bf16 or fp16"};
@@ -446,9 +447,8 @@ lm_status lionmuon_grouped_workspace_bytes(int64_t rows, int64_t count, int64_t 
                                            size_t* out_bytes) {
   return guarded("lionmuon_grouped_workspace_bytes", [&]() -> hipError_t {
     need(out_bytes != nullptr, "null output");
-    need(rows >= 0 && rows < (int64_t(1) << 30) && count >= 1 && count <= (int64_t(1) << 20) && n >= 1 && k >= 1 &&
-             n < kMaxLd && k < kMaxLd,
-         "bad size");
+    need(rows >= 0 && rows < kMaxGroupedRows && count >= 1 && n >= 1 && k >= 1 && n < kMaxLd && k < kMaxLd, "bad size");
+    if (count > LM_GROUPED_MAX_EXPERTS) throw Bad{LM_ERR_UNSUPPORTED, "too many experts"};
     *out_bytes = partial_bytes(rows, count, n, k);
     return hipSuccess;
   });

@@ -124,12 +124,14 @@ __device__ __forceinline__ Groups groups_from(const int32_t* offsets, int expert
   g.upto = wave_scan(i < experts ? max((max(g.end - g.first, 0) + bm - 1) / bm, least) : 0);
   return g;
 }
-// All groups; *last: the last 64 experts', all of them where there are no more.
+// All groups, at most as many as a rising sequence of offsets can make (others count
+// no further); *last: the last 64 experts', all of them where there are no more.
 __device__ __forceinline__ int count_groups(const int32_t* offsets, int experts, int rows, int bm, int least, Groups* last) {
+  const int most = rows / bm + (least > 0 ? experts : min(experts, rows));
   int total = 0;
   for (int base = 0; base < experts; base += 64) {
     *last = groups_from(offsets, experts, rows, bm, least, base);
-    total += __builtin_amdgcn_readlane(last->upto, 63);
+    total = min(total + __builtin_amdgcn_readlane(last->upto, 63), most);
   }
   return total;
 }

@@ -283,12 +283,16 @@ def test_binding_refuses_host_tensors_and_wrong_kinds():
 
 
 def test_products_too_large_for_a_launch_are_refused(lib):
-    w = stack(1, 1 << 20, 4096, 64)
-    refused(lib, lib.lionmuon_grouped_product(mat(0, 1 << 26, 64), w, at(2), mat(3, 1 << 26, 4096), None),
+    w = stack(1, 1 << 16, 16384, 64)
+    refused(lib, lib.lionmuon_grouped_product(mat(0, 1 << 26, 64), w, at(2), mat(3, 1 << 26, 16384), None),
             UNSUPPORTED, "tiles")
-    refused(lib, lib.lionmuon_grouped_weight_grad(mat(0, 8, 4096), mat(4, 8, 64), None, at(2),
-                                                  stack(1, 1 << 20, 4096, 64, dtype=F32), 0, None, 0, None),
+    refused(lib, lib.lionmuon_grouped_weight_grad(mat(0, 8, 16384), mat(4, 8, 64), None, at(2),
+                                                  stack(1, 1 << 16, 16384, 64, dtype=F32), 0, None, 0, None),
             UNSUPPORTED, "tiles")
+    refused(lib, lib.lionmuon_grouped_product(mat(0, 8, 64), stack(1, (1 << 16) + 1, 8, 64), at(2),
+                                              mat(3, 8, 8), None), UNSUPPORTED, "experts")
+    refused(lib, lib.lionmuon_grouped_product(mat(0, 1 << 30, 64), stack(1, 1, 8, 64), at(2),
+                                              mat(3, 1 << 30, 8), None), BAD, "rows")
 
 
 def test_checkpoint_with_a_short_last_row_of_scales_is_refused():
