@@ -2,16 +2,84 @@
 // and root-mean-square norms with their gradients (include/lionmuon_grad.h).
 // All of them are bound by HBM: each reads its inputs and writes its outputs once.
 //
-// A lane takes eight consecutive elements; the 16 lanes of a DPP row are the
-// 128 columns that share a scale, so a checkpoint's maximum is four lane
-// rotations away, without LDS, and every kernel that has a tensor in registers
-// can store its checkpoint on the way.
+// A lane takes eight elements; the 16 lanes of a DPP row are the 128 columns that
+// share a scale, so a checkpoint's maximum is four lane rotations away, without
+// LDS, and every kernel that has a tensor in registers can store its checkpoint
+// on the way. 32768 x 4096 in bf16: checkpoint 5.3 TB/s, restore 6.9, norm 5.2, its
+// gradient 5.4, activations and their gradients 5.4 to 5.9 (a large copy: 5.15 to 5.5).
 #include <type_traits>
 
 #include "grad_device.h"
 
 namespace lm {
 namespace {
+
+// Columns of a lane: eight in a row in 16-bit types, two fours 64 apart in fp32, so
+// that the 16 bytes of neighbouring lanes are neighbours in either and an access
+// covers whole lines (fp32, 32768 x 4096: gated activation's gradient from a checkpoint
+// 5.3 TB/s, restore 7.0; by 32 bytes a lane 3.6 and 3.2).
+template <typename T> constexpr bool kFours = sizeof(T) == 4;
+template <typename T>
+__device__ __forceinline__ int column(int l) {      // the first one; l counts the lanes of a row
+  return kFours<T> ? (l >> 4) * kCkptBlock + (l & 15) * 4 : l * 8;
+}
+
+// Eight values of E laid out as a kernel for T has them: N at a time. The 16-byte
+// accesses are unaligned ones as far as the compiler knows (the hardware takes
+// any address, and aligned ones at full speed), so one path serves every stride;
+// only the last elements of a row go one at a time. n: columns from p to the row's end.
+template <typename E, bool FOURS>
+__device__ __forceinline__ void load8(const E* p, int64_t n, E v[8]) {
+  constexpr int N = FOURS ? 4 : 8;
+#pragma unroll
+  for (int h = 0; h < 8; h += N) {
+    const int64_t left = n - (h ? 64 : 0);
+    const E* q = p + (h ? 64 : 0);
+    if (left >= N) {
+      __builtin_memcpy(v + h, q, N * sizeof(E));
+    } else {
+#pragma unroll
+      for (int j = 0; j < N; ++j) v[h + j] = j < left ? q[j] : E(0.0f);
+    }
+  }
+}
+
+// Results leave with the non-temporal hint: a wave writes whole lines of tensors
+// that no cache on the way will be asked for (32768 x 4096 bf16 from a checkpoint:
+// 112 us without, 58 with it; gated activation's gradient 314 -> 230). In fp32 16 lanes write
+// 256 bytes and leave a gap as long: only where those begin with a line (20000 x 1003
+// from a checkpoint: 29 us with the hint, 17 without).
+template <typename E, bool FOURS>
+__device__ __forceinline__ void store8(E* p, int64_t n, const float v[8]) {
+  constexpr int N = FOURS ? 4 : 8;
+#pragma unroll
+  for (int h = 0; h < 8; h += N) {
+    const int64_t left = n - (h ? 64 : 0);
+    E* q = p + (h ? 64 : 0);
+    if (left >= N) {
+      E t[N];
+#pragma unroll
+      for (int j = 0; j < N; ++j) t[j] = E(v[h + j]);
+      u32x4 x;
+      if constexpr (N * sizeof(E) == 16) {
+        __builtin_memcpy(&x, t, 16);
+        if (!FOURS || ((reinterpret_cast<uintptr_t>(q) - (threadIdx.x & 15) * 16) & 127) == 0) {
+          store16_nt(q, x);
+        } else {
+          asm volatile("" ::: "memory");      // (merged with the other store, neither would have the hint)
+          __builtin_memcpy(q, t, 16);
+          asm volatile("" ::: "memory");
+        }
+      } else {
+        __builtin_memcpy(q, t, sizeof(t));      // (32 bytes: half lines, which the hint makes slower)
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < N; ++j)
+        if (j < left) q[j] = E(v[h + j]);
+    }
+  }
+}
 
 // Maximum over the 16 lanes of a DPP row, in all of them.
 template <int CTRL>
@@ -56,9 +124,16 @@ __device__ __forceinline__ uint32_t encode8(const float v[8], u32x2* codes) {
 // Columns a row of codes is written to: the next multiple of 16.
 __device__ __forceinline__ int64_t padded16(int64_t cols) { return (cols + 15) & ~int64_t(15); }
 
-// Store the codes of columns c .. c + 7 of a row and, from a block's first lane, its scale.
+// Store the codes of a lane's columns, from c on, and, from a block's first lane, its scale.
+template <typename T>
 __device__ __forceinline__ void put8(const CkptView& k, int64_t row, int64_t c, int64_t cols, u32x2 codes, uint32_t scale) {
-  if (c < padded16(cols)) *reinterpret_cast<u32x2*>(k.codes + row * k.ld_codes + c) = codes;
+  uint8_t* p = k.codes + row * k.ld_codes + c;
+  if constexpr (kFours<T>) {
+    if (c < padded16(cols)) *reinterpret_cast<uint32_t*>(p) = codes[0];
+    if (c + 64 < padded16(cols)) *reinterpret_cast<uint32_t*>(p + 64) = codes[1];
+  } else {
+    if (c < padded16(cols)) *reinterpret_cast<u32x2*>(p) = codes;
+  }
   if ((c & (kCkptBlock - 1)) == 0 && c < cols) k.scales[row * k.ld_scales + c / kCkptBlock] = uint8_t(scale);
 }
 
@@ -88,9 +163,8 @@ BlockWalk walk_of(int64_t rows, int64_t cols) {
   return w;
 }
 
-// load(row, column) gives what a lane needs of its eight columns, use(row, column,
-// that) does the rest: a group has the loads of two blocks in flight.
-template <class L, class U>
+// load(row, column) gives what a lane needs of its columns, use(row, column, that) does the rest: a group has the loads of two blocks in flight.
+template <typename T, class L, class U>
 __device__ __forceinline__ void for_blocks(const BlockWalk& w, L load, U use) {
   constexpr int kGroups = kRowThreads / 16;
   const int64_t row0 = int64_t(blockIdx.x) * w.per;
@@ -99,7 +173,7 @@ __device__ __forceinline__ void for_blocks(const BlockWalk& w, L load, U use) {
   auto place = [&](int i, int64_t* row, int64_t* c) {
     const int r = i / w.blocks;
     *row = row0 + r;
-    *c = int64_t(i - r * w.blocks) * kCkptBlock + (threadIdx.x & 15) * 8;
+    *c = int64_t(i - r * w.blocks) * kCkptBlock + column<T>(threadIdx.x & 15);
   };
   for (int i = threadIdx.x >> 4; i < total; i += 2 * kGroups) {
     int64_t r0, c0, r1, c1;
@@ -114,69 +188,74 @@ __device__ __forceinline__ void for_blocks(const BlockWalk& w, L load, U use) {
   }
 }
 
-// What is loaded of eight values, before it is converted.
+// What is loaded of a lane's values, before it is converted.
 template <typename T>
 struct Raw {
   T v[8];
-  __device__ __forceinline__ void load(const T* p, int64_t n) {
-    if (n >= 8) {
-      __builtin_memcpy(v, p, sizeof(v));
-    } else {
-#pragma unroll
-      for (int j = 0; j < 8; ++j) v[j] = j < n ? p[j] : T(0.0f);
-    }
-  }
+  __device__ __forceinline__ void load(const T* p, int64_t n) { load8<T, kFours<T>>(p, n, v); }
   __device__ __forceinline__ void get(float o[8]) const {
 #pragma unroll
     for (int j = 0; j < 8; ++j) o[j] = float(v[j]);
   }
 };
-// Eight codes of a checkpoint from column c on, with the scale of their block. ANY: c
-// need not be a multiple of 8, and the codes may lie in two blocks.
-template <bool ANY = false>
+// The codes of a lane's columns, from c on, with the scale of their block. ANY: c may
+// be any column, and each run of codes may lie in two blocks.
+template <typename T, bool ANY = false>
 struct RawCodes {
+  static constexpr int N = kFours<T> ? 4 : 8, kRuns = 8 / N, kScales = ANY ? kRuns : 1;
   u32x2 w;
-  uint32_t s0, s1;
-  int edge;            // codes of the first block
+  uint32_t s0[kScales], s1[kScales];
+  int edge[kScales];   // codes of a run's first block
   __device__ __forceinline__ void load(const CkptView& k, int64_t row, int64_t c, int64_t n) {
     w = u32x2{0u, 0u};
-    s0 = s1 = 0;
-    edge = 8;
-    if (n <= 0) return;
-    const uint8_t* p = k.codes + row * k.ld_codes + c;
-    if (!ANY) {
-      // (rows of codes reach to a multiple of 16)
-      w = *reinterpret_cast<const u32x2*>(p);
-    } else if (n >= 8) {
-      __builtin_memcpy(&w, p, 8);
-    } else {
 #pragma unroll
-      for (int j = 0; j < 8; ++j)
-        if (j < n) w[j >> 2] |= uint32_t(p[j]) << (8 * (j & 3));
+    for (int h = 0; h < kScales; ++h) {
+      s0[h] = s1[h] = 0;
+      edge[h] = N;
     }
     const uint8_t* s = k.scales + row * k.ld_scales;
-    const int64_t b0 = c / kCkptBlock;
-    s0 = s[b0];
-    if constexpr (ANY) {
-      s1 = s[(c + (n < 8 ? n : 8) - 1) / kCkptBlock];
-      edge = int((b0 + 1) * kCkptBlock - c);
+#pragma unroll
+    for (int h = 0; h < kRuns; ++h) {
+      const int64_t left = n - 64 * h, at = c + 64 * h;
+      if (left <= 0) continue;
+      const uint8_t* p = k.codes + row * k.ld_codes + at;
+      uint32_t t[N / 4];
+      if (!ANY) {
+        // (rows of codes reach to a multiple of 16)
+        __builtin_memcpy(t, __builtin_assume_aligned(p, N), N);
+      } else if (left >= N) {
+        __builtin_memcpy(t, p, N);
+      } else {
+#pragma unroll
+        for (int i = 0; i < N / 4; ++i) t[i] = 0;
+#pragma unroll
+        for (int j = 0; j < N; ++j)
+          if (j < left) t[j >> 2] |= uint32_t(p[j]) << (8 * (j & 3));
+      }
+#pragma unroll
+      for (int i = 0; i < N / 4; ++i) w[h * (N / 4) + i] = t[i];
+      const int64_t b0 = at / kCkptBlock;
+      if (h < kScales) s0[h] = s[b0];
+      if constexpr (ANY) {
+        s1[h] = s[(at + (left < N ? left : N) - 1) / kCkptBlock];
+        edge[h] = int((b0 + 1) * kCkptBlock - at);
+      }
     }
   }
   __device__ __forceinline__ void get(float o[8]) const {
     if constexpr (ANY) {
       decode8(w, 1.0f, o);
-      const float f0 = scale_of(s0), f1 = scale_of(s1);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) o[j] *= j < edge ? f0 : f1;
+      for (int j = 0; j < 8; ++j) o[j] *= scale_of(j % N < edge[j / N] ? s0[j / N] : s1[j / N]);
     } else {
-      decode8(w, scale_of(s0), o);
+      decode8(w, scale_of(s0[0]), o);
     }
   }
 };
 
 template <typename T>
 __global__ __launch_bounds__(kRowThreads) void checkpoint_kernel(BlockWalk w, MatView x, CkptView out) {
-  for_blocks(w, [&](int64_t row, int64_t c) {
+  for_blocks<T>(w, [&](int64_t row, int64_t c) {
     Raw<T> d;
     d.load(static_cast<const T*>(x.data) + row * x.ld + c, w.cols - c);
     return d;
@@ -185,20 +264,20 @@ __global__ __launch_bounds__(kRowThreads) void checkpoint_kernel(BlockWalk w, Ma
     d.get(v);
     u32x2 codes;
     const uint32_t s = encode8(v, &codes);
-    put8(out, row, c, w.cols, codes, s);
+    put8<T>(out, row, c, w.cols, codes, s);
   });
 }
 
 template <typename T>
 __global__ __launch_bounds__(kRowThreads) void restore_kernel(BlockWalk w, CkptView k, MatView out) {
-  for_blocks(w, [&](int64_t row, int64_t c) {
-    RawCodes<> d;
+  for_blocks<T>(w, [&](int64_t row, int64_t c) {
+    RawCodes<T> d;
     d.load(k, row, c, w.cols - c);
     return d;
-  }, [&](int64_t row, int64_t c, const RawCodes<>& d) {
+  }, [&](int64_t row, int64_t c, const RawCodes<T>& d) {
     float v[8];
     d.get(v);
-    store8(static_cast<T*>(out.data) + row * out.ld + c, w.cols - c, v);
+    store8<T, kFours<T>>(static_cast<T*>(out.data) + row * out.ld + c, w.cols - c, v);
   });
 }
 
@@ -227,7 +306,7 @@ __global__ __launch_bounds__(kRowThreads) void activation_kernel(BlockWalk w, Ma
     Raw<T> x, u;
   };
   const int64_t cols = w.cols;
-  for_blocks(w, [&](int64_t row, int64_t c) {
+  for_blocks<T>(w, [&](int64_t row, int64_t c) {
     const T* p = static_cast<const T*>(a.data) + row * a.ld + c;
     Data d;
     d.x.load(p, cols - c);
@@ -242,13 +321,13 @@ __global__ __launch_bounds__(kRowThreads) void activation_kernel(BlockWalk w, Ma
     if constexpr (KEEP) {
       u32x2 codes;
       uint32_t s = encode8(x, &codes);
-      put8(kept, row, c, cols, codes, s);
+      put8<T>(kept, row, c, cols, codes, s);
       if constexpr (KIND == kSwiglu) {
         s = encode8(u, &codes);
-        put8(kept, row, cols + c, 2 * cols, codes, s);
+        put8<T>(kept, row, cols + c, 2 * cols, codes, s);
       }
     }
-    store8(static_cast<T*>(h.data) + row * h.ld + c, cols - c, o);
+    store8<T, kFours<T>>(static_cast<T*>(h.data) + row * h.ld + c, cols - c, o);
   });
 }
 
@@ -260,12 +339,12 @@ __global__ __launch_bounds__(kRowThreads) void activation_grad_kernel(BlockWalk 
   };
   struct Kept {
     Raw<T> d;
-    RawCodes<> x;
-    RawCodes<true> u;          // its half may start anywhere
+    RawCodes<T> x;
+    RawCodes<T, true> u;          // its half may start anywhere
   };
   using Data = std::conditional_t<KEPT, Kept, Whole>;
   const int64_t cols = w.cols;
-  for_blocks(w, [&](int64_t row, int64_t c) {
+  for_blocks<T>(w, [&](int64_t row, int64_t c) {
     const int64_t n = cols - c;
     Data d;
     d.d.load(static_cast<const T*>(dh.data) + row * dh.ld + c, n);
@@ -301,9 +380,9 @@ __global__ __launch_bounds__(kRowThreads) void activation_grad_kernel(BlockWalk 
       }
     }
     T* q = static_cast<T*>(da.data) + row * da.ld + c;
-    store8(q, n, dx);
-    if constexpr (KIND == kSwiglu) store8(q + cols, n, du);
-    if (h.data) store8(static_cast<T*>(h.data) + row * h.ld + c, n, o);
+    store8<T, kFours<T>>(q, n, dx);
+    if constexpr (KIND == kSwiglu) store8<T, kFours<T>>(q + cols, n, du);
+    if (h.data) store8<T, kFours<T>>(static_cast<T*>(h.data) + row * h.ld + c, n, o);
   });
 }
 
@@ -353,8 +432,8 @@ __global__ __launch_bounds__(team_threads<NT>()) void rmsnorm_kernel(NormArgs a)
   float w[C][8];
 #pragma unroll
   for (int i = 0; i < C; ++i) {
-    const int c = (lane + i * NT) * 8;
-    load8(a.weight + c, cols - c, w[i]);
+    const int c = column<T>(lane + i * NT);
+    load8<float, kFours<T>>(a.weight + c, cols - c, w[i]);
   }
   int parity = 0;
   for (int64_t row = int64_t(blockIdx.x) * kTeams + team; row < a.rows; row += int64_t(gridDim.x) * kTeams) {
@@ -362,20 +441,20 @@ __global__ __launch_bounds__(team_threads<NT>()) void rmsnorm_kernel(NormArgs a)
     Raw<T> x[C], r[C];
 #pragma unroll
     for (int i = 0; i < C; ++i) {
-      const int c = (lane + i * NT) * 8, n = cols - c;
+      const int c = column<T>(lane + i * NT), n = cols - c;
       x[i].load(static_cast<const T*>(a.x.data) + row * a.x.ld + c, n);
       if (a.residual.data) r[i].load(static_cast<const T*>(a.residual.data) + row * a.residual.ld + c, n);
     }
     float ss = 0.0f;
 #pragma unroll
     for (int i = 0; i < C; ++i) {
-      const int c = (lane + i * NT) * 8, n = cols - c;
+      const int c = column<T>(lane + i * NT), n = cols - c;
       x[i].get(v[i]);
       if (a.residual.data) {
         // rounded as it is stored: the backward pass sees the same stream
 #pragma unroll
         for (int j = 0; j < 8; ++j) v[i][j] = float(T(v[i][j] + float(r[i].v[j])));
-        if (a.sum.data) store8(static_cast<T*>(a.sum.data) + row * a.sum.ld + c, n, v[i]);
+        if (a.sum.data) store8<T, kFours<T>>(static_cast<T*>(a.sum.data) + row * a.sum.ld + c, n, v[i]);
       }
 #pragma unroll
       for (int j = 0; j < 8; ++j) ss = fmaf(v[i][j], v[i][j], ss);
@@ -386,14 +465,19 @@ __global__ __launch_bounds__(team_threads<NT>()) void rmsnorm_kernel(NormArgs a)
     if (a.rstd && lane == 0) a.rstd[row] = rstd;
 #pragma unroll
     for (int i = 0; i < C; ++i) {
-      const int c = (lane + i * NT) * 8, n = cols - c;
+      const int c = column<T>(lane + i * NT), n = cols - c;
 #pragma unroll
       for (int j = 0; j < 8; ++j) v[i][j] = v[i][j] * rstd * w[i][j];
-      if (a.y.data) store8(static_cast<T*>(a.y.data) + row * a.y.ld + c, n, v[i]);
+      if (a.y.data) store8<T, kFours<T>>(static_cast<T*>(a.y.data) + row * a.y.ld + c, n, v[i]);
       if (a.kept.codes) {
+        if (n < (kFours<T> ? 68 : 8)) {      // (0 behind the last column, in a row of NaN too)
+#pragma unroll
+          for (int j = 0; j < 8; ++j)
+            if (j + (kFours<T> && j > 3 ? 60 : 0) >= n) v[i][j] = 0.0f;
+        }
         u32x2 codes;
         const uint32_t s = encode8(v[i], &codes);
-        put8(a.kept, row, c, cols, codes, s);
+        put8<T>(a.kept, row, c, cols, codes, s);
       }
     }
   }
@@ -411,8 +495,8 @@ __global__ __launch_bounds__(team_threads<NT>()) void rmsnorm_grad_kernel(NormAr
   float w[C][8], dw[C][8];
 #pragma unroll
   for (int i = 0; i < C; ++i) {
-    const int c = (lane + i * NT) * 8;
-    load8(a.weight + c, cols - c, w[i]);
+    const int c = column<T>(lane + i * NT);
+    load8<float, kFours<T>>(a.weight + c, cols - c, w[i]);
 #pragma unroll
     for (int j = 0; j < 8; ++j) dw[i][j] = 0.0f;
   }
@@ -420,11 +504,11 @@ __global__ __launch_bounds__(team_threads<NT>()) void rmsnorm_grad_kernel(NormAr
   for (int64_t row = int64_t(blockIdx.x) * kTeams + team; row < a.rows; row += int64_t(gridDim.x) * kTeams) {
     const float rstd = a.rstd[row];
     // (kept as loaded and converted twice: half the registers of the values)
-    std::conditional_t<KEPT, RawCodes<>, Raw<T>> h[C];
+    std::conditional_t<KEPT, RawCodes<T>, Raw<T>> h[C];
     Raw<T> d[C], r[C];
 #pragma unroll
     for (int i = 0; i < C; ++i) {
-      const int c = (lane + i * NT) * 8, n = cols - c;
+      const int c = column<T>(lane + i * NT), n = cols - c;
       if constexpr (KEPT) h[i].load(a.kept, row, c, n);
       else h[i].load(static_cast<const T*>(a.s.data) + row * a.s.ld + c, n);
       d[i].load(static_cast<const T*>(a.dy.data) + row * a.dy.ld + c, n);
@@ -447,13 +531,13 @@ __global__ __launch_bounds__(team_threads<NT>()) void rmsnorm_grad_kernel(NormAr
       parity ^= 1;
 #pragma unroll
       for (int i = 0; i < C; ++i) {
-        const int c = (lane + i * NT) * 8, n = cols - c;
+        const int c = column<T>(lane + i * NT), n = cols - c;
         float x[8], o[8];
         h[i].get(x);
 #pragma unroll
         for (int j = 0; j < 8; ++j)
           o[j] = fmaf(rstd, fmaf(-(x[j] * rstd), dot, float(d[i].v[j]) * w[i][j]), a.residual_grad.data ? float(r[i].v[j]) : 0.0f);
-        store8(static_cast<T*>(a.dx.data) + row * a.dx.ld + c, n, o);
+        store8<T, kFours<T>>(static_cast<T*>(a.dx.data) + row * a.dx.ld + c, n, o);
       }
     }
   }
@@ -477,8 +561,8 @@ __global__ __launch_bounds__(team_threads<NT>()) void rmsnorm_grad_kernel(NormAr
   float* out = a.partial + int64_t(blockIdx.x) * cols;
 #pragma unroll
   for (int i = 0; i < C; ++i) {
-    const int c = (lane + i * NT) * 8;
-    store8(out + c, cols - c, dw[i]);
+    const int c = column<T>(lane + i * NT);
+    store8<float, kFours<T>>(out + c, cols - c, dw[i]);
   }
 }
 

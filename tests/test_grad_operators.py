@@ -262,6 +262,21 @@ def test_norm_in_place_forms_and_zero_rows():
     assert (y == 0).all() and torch.allclose(rstd, torch.full_like(rstd, 1e3))
 
 
+@pytest.mark.parametrize("dtype", ["fp32", "bf16", "fp16"])
+@pytest.mark.parametrize("cols", [1, 5, 67, 131, 1003])
+def test_bytes_behind_the_last_code_are_zero_in_rows_of_nan_too(cols, dtype):
+    x = make((5, cols), TYPES[dtype], cols)
+    x[1, 0], x[3, cols - 1] = float("nan"), float("inf")
+    w = torch.ones(cols, device="cuda")
+    ld = -(-cols // 16) * 16
+    for write in (lambda k: gr.lionmuon_checkpoint(x, out=k),
+                  lambda k: gr.lionmuon_rmsnorm(x, w, checkpoint=k),
+                  lambda k: gr.lionmuon_activation(x, "gelu", checkpoint=k)):
+        codes = torch.full((5, ld), 9, dtype=torch.uint8, device="cuda")
+        write(gr.Checkpoint(codes[:, :cols], torch.zeros(5, -(-cols // 128), dtype=torch.uint8, device="cuda")))
+        assert (codes[:, cols:] == 0).all()
+
+
 def test_norm_gradient_against_differences():
     rows, cols, eps = 5, 24, 1e-5
     s, dy = make((rows, cols), torch.float32, 1), make((rows, cols), torch.float32, 2)
