@@ -390,8 +390,8 @@ __global__ __launch_bounds__(kRowThreads) void activation_grad_kernel(BlockWalk 
 // Root-mean-square norm
 // ---------------------------------------------------------------------------
 // NT lanes share a row and hold it in registers, C times eight elements each:
-// a wave for rows of up to 1536 columns (four rows to a workgroup, no
-// barrier), 256 or 1024 threads for longer ones. A team walks rows with the
+// a wave for short rows (four rows to a workgroup, no barrier), 256 or 1024
+// threads for longer ones. A team walks rows with the
 // stride of the grid, so that the weights are read once a team.
 // (by lane rotations within 16 lanes, then one value of each 16: no LDS)
 template <int CTRL>
@@ -601,21 +601,29 @@ template <int V> struct Int {
   static constexpr int value = V;
 };
 
+// Columns of the rows that a wave takes by itself. The gradient holds three tensors
+// and the weights' sums, and with three chunks of each too few waves fit a CU
+// (32768 x 1280 bf16: 84 us by waves, 67 by workgroups of 256).
+template <bool GRAD> constexpr int kWaveCols = GRAD ? 1024 : 1536;
+
 // Lanes of a row's team and their chunks for rows of `cols` columns.
-template <class F>
+template <bool GRAD, class F>
 void with_team(int cols, F f) {
-  if (cols <= 512) f(Int<64>(), Int<1>());
-  else if (cols <= 1024) f(Int<64>(), Int<2>());
-  else if (cols <= 1536) f(Int<64>(), Int<3>());
-  else if (cols <= 2048) f(Int<256>(), Int<1>());
-  else if (cols <= 4096) f(Int<256>(), Int<2>());
-  else if (cols <= 8192) f(Int<256>(), Int<4>());
-  else f(Int<1024>(), Int<2>());
+  if (cols <= 512) return f(Int<64>(), Int<1>());
+  if (cols <= 1024) return f(Int<64>(), Int<2>());
+  if constexpr (kWaveCols<GRAD> == 1536) {
+    if (cols <= 1536) return f(Int<64>(), Int<3>());
+  }
+  if (cols <= 2048) return f(Int<256>(), Int<1>());
+  if (cols <= 4096) return f(Int<256>(), Int<2>());
+  if (cols <= 8192) return f(Int<256>(), Int<4>());
+  f(Int<1024>(), Int<2>());
 }
 
 // Workgroups of a norm: a row of the grid a team until every CU has eight.
+template <bool GRAD>
 int64_t norm_groups(int64_t rows, int cols) {
-  const int64_t teams = cols <= 1536 ? 4 : 1;
+  const int64_t teams = cols <= kWaveCols<GRAD> ? 4 : 1;
   const int64_t all = (rows + teams - 1) / teams, most = cols <= 8192 ? 2048 : 512;
   return all < most ? all : most;
 }
@@ -674,10 +682,10 @@ hipError_t launch_activation_grad(Elem t, int kind, MatView dh, MatView a, CkptV
 }
 
 hipError_t launch_rmsnorm(Elem t, const NormArgs& a, hipStream_t stream) {
-  const dim3 grid(unsigned(norm_groups(a.rows, a.cols)));
+  const dim3 grid(unsigned(norm_groups<false>(a.rows, a.cols)));
   return with_type(t, [&](auto el) {
     using T = decltype(el);
-    with_team(a.cols, [&](auto nt, auto c) {
+    with_team<false>(a.cols, [&](auto nt, auto c) {
       constexpr int kNT = decltype(nt)::value, kC = decltype(c)::value;
       rmsnorm_kernel<T, kNT, kC><<<grid, team_threads<kNT>(), 0, stream>>>(a);
     });
@@ -685,7 +693,7 @@ hipError_t launch_rmsnorm(Elem t, const NormArgs& a, hipStream_t stream) {
 }
 
 int64_t rmsnorm_grad_groups(int64_t rows, int64_t cols) {
-  const int64_t g = norm_groups(rows, int(cols)), most = cols <= 8192 ? 1024 : 256;
+  const int64_t g = norm_groups<true>(rows, int(cols)), most = cols <= 8192 ? 1024 : 256;
   return g < most ? g : most;
 }
 
@@ -695,7 +703,7 @@ hipError_t launch_rmsnorm_grad(Elem t, const NormArgs& a, hipStream_t stream) {
   if (groups > 0) {
     e = with_type(t, [&](auto el) {
       using T = decltype(el);
-      with_team(a.cols, [&](auto nt, auto c) {
+      with_team<true>(a.cols, [&](auto nt, auto c) {
         constexpr int kNT = decltype(nt)::value, kC = decltype(c)::value;
         if (a.kept.codes) rmsnorm_grad_kernel<T, kNT, kC, true><<<dim3(groups), team_threads<kNT>(), 0, stream>>>(a);
         else rmsnorm_grad_kernel<T, kNT, kC, false><<<dim3(groups), team_threads<kNT>(), 0, stream>>>(a);
