@@ -960,6 +960,12 @@ struct WeightProduct {
 // and needs 2 rows / part + 1 in all.
 __device__ __forceinline__ int partial_slot(int first, int part) { return int(2 * int64_t(first) / part); }
 
+// 256 x 128 at most: the second set of sums (FOLD) takes as many registers as the
+// first. Eight waves of 64 x 64 read 128 KB of LDS a stage and copy 48 KB into it, about
+// 1400 of its 2000 cycles; that and the power limit bound it (8192^3: 1080 TFLOP/s; 32768 x
+// 1280 x 5120: 450 us). From a checkpoint the codes' way through LDS adds 32 KB (515 us).
+// Experts one after the other instead of the longest first: 16384 x 4096 x 1024 by eight
+// skewed ones twice as long.
 template <typename T, int MB, class S, bool DA, bool DB>
 __global__ __launch_bounds__(S::kThreads, S::kWorkgroups) void weight_product_kernel(WeightProduct g) {
   using K = Tile<T, kCols, MB, S, DA, DB>;
