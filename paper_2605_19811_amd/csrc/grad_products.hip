@@ -274,8 +274,10 @@ struct Tile {
         d = descriptor(s.p + int64_t(k0) * 2, s.rows > 0 ? (s.rows - 1) * s.ld + int64_t(s.depth - k0) * 2 : 0);
         if (k0 + first >= s.depth) at = kOutside;
       } else {
+        // (to the end of the last column's dword: the range check drops a dword
+        // that reaches past the descriptor's end, and with it an odd last column)
         const int left = min(s.depth - k0, KS);
-        d = descriptor(s.p + int64_t(k0) * s.ld, left > 0 ? (left - 1) * s.ld + int64_t(s.cols) * 2 : 0);
+        d = descriptor(s.p + int64_t(k0) * s.ld, left > 0 ? (left - 1) * s.ld + (int64_t(s.cols) + 1) / 2 * 4 : 0);
       }
     }
     __device__ __forceinline__ void copy(int q, uint32_t dst) const {      // dst: LDS address of the wave's first copy

@@ -626,3 +626,35 @@ def test_weight_gradient_from_a_checkpoint_is_that_of_its_values(experts, rows, 
     wide[:, 1:1 + kept.scales.shape[1]] = kept.scales
     odd = gr.Checkpoint(kept.codes, wide[:, 1:1 + kept.scales.shape[1]])
     assert float((gr.lionmuon_grouped_weight_grad(dy, odd, offsets) - got).norm() / got.norm()) < 1e-6
+
+
+# -- rows 16-byte aligned, widths that are not --------------------------------
+def aligned_rows(rows, cols, dt, seed):
+    """Random (rows, cols) tensor whose rows start 16-byte aligned; what lies between
+    them is NaN."""
+    g = torch.Generator().manual_seed(seed)
+    buf = torch.full((rows, cols // 8 * 8 + 8), float("nan"), dtype=dt, device="cuda")
+    buf[:, :cols] = torch.randn(rows, cols, generator=g).to(dt).cuda()
+    return buf[:, :cols]
+
+
+# every width modulo eight, by each of the tile sizes of the two gradients, rows of several stages
+@pytest.mark.parametrize("rows,sizes,n,k", [(200, [200], 144, 64), (300, [100, 200], 296, 296),
+                                            (4000, [1333, 2667], 1024, 768), (4200, [4200], 4096, 1024)])
+@pytest.mark.parametrize("extra", range(1, 8))
+def test_last_columns_of_widths_off_16_bytes_in_aligned_rows(rows, sizes, n, k, extra):
+    dt, experts = torch.bfloat16, len(sizes)
+    n, k = n + extra, k + extra
+    x, dy, w = (aligned_rows(r, c, dt, s) for r, c, s in ((rows, k, 1), (rows, n, 2), (experts * n, k, 3)))
+    w = torch.as_strided(w, (experts, n, k), (n * w.stride(0), w.stride(0), 1))
+    at = np.concatenate([[0], np.cumsum(sizes)])
+    offsets = torch.tensor(at, dtype=torch.int32, device="cuda")
+    dx, dw = gr.lionmuon_grouped_input_grad(dy, w, offsets), gr.lionmuon_grouped_weight_grad(dy, x, offsets)
+    y = gr.lionmuon_grouped_product(x, w, offsets)
+    for e in range(experts):
+        r = slice(int(at[e]), int(at[e + 1]))
+        a, b, c = dy[r].double(), w[e].double(), x[r].double()
+        for got, p, q, hs in ((dx[r], a, b, half_step(dt)), (y[r], c, b.t(), half_step(dt)), (dw[e], a.t(), c, 0.0)):
+            want, mag = p @ q, p.abs() @ q.abs()
+            err = (got.double() - want).abs()
+            assert (err <= hs * 1.01 * want.abs() + sum_bound(p.shape[1]) * mag).all()
