@@ -90,7 +90,9 @@ class Checkpoint:
     """8-bit checkpoint of a (rows, cols) tensor: e4m3 ``codes`` (uint8, rows
     16-byte aligned and a multiple of 16 bytes apart) and ``scales`` (uint8, one
     byte e + 127 for each 128 columns of a row); a code stands for its
-    e4m3 value times 2^e."""
+    e4m3 value times 2^e. Each row of codes reaches to a multiple of 16 bytes (the
+    operators write 0 behind the last code): ``codes`` are the first columns of a
+    tensor with such rows."""
 
     __slots__ = ("shape", "device", "_desc", "_buffer", "_codes", "_scales")
 
@@ -110,6 +112,11 @@ class Checkpoint:
         ld_scales, step_scales = scales.stride()
         if (cols > 1 and step != 1) or (blocks > 1 and step_scales != 1):
             _invalid("the rows of codes and scales must be contiguous")
+        # a row's codes are written to the next multiple of 16: bytes of that row
+        whole = -(-cols // 16) * 16
+        if whole > cols and rows and (
+                ld < whole or (rows - 1) * ld + whole > codes.untyped_storage().nbytes() - codes.storage_offset()):
+            _invalid("the rows of codes must reach to a multiple of 16 bytes, the last one too")
         if rows > 1 and ld_scales % 4 == 0 and rows * ld_scales > \
                 scales.untyped_storage().nbytes() - scales.storage_offset():
             _invalid("the last row of scales must be as long as the others")
@@ -119,7 +126,7 @@ class Checkpoint:
         self._codes = codes
         self._scales = scales
         self._desc = lm_checkpoint(codes.data_ptr(), scales.data_ptr(), rows, cols,
-                                   ld if rows > 1 else -(-cols // 16) * 16,
+                                   ld if rows > 1 else whole,
                                    ld_scales if rows > 1 else blocks)
 
     @classmethod

@@ -302,3 +302,36 @@ def test_checkpoint_with_a_short_last_row_of_scales_is_refused():
     with pytest.raises(lm.LionMuonError):
         gr.Checkpoint(torch.zeros(2, 384, dtype=u8), scales)
     gr.Checkpoint(torch.zeros(2, 384, dtype=u8), torch.as_strided(torch.zeros(8, dtype=u8), (2, 3), (4, 1)))
+
+
+def test_checkpoint_with_codes_that_end_inside_16_bytes_is_refused():
+    """Writers put 0 behind a row's last code up to a multiple of 16 bytes: these
+    have to be bytes of that row, in a single row and in the last one too."""
+    import torch
+    u8 = torch.uint8
+
+    def make(codes):
+        return gr.Checkpoint(codes, torch.zeros(codes.shape[0], -(-codes.shape[1] // 128), dtype=u8))
+
+    large = torch.zeros(4096, dtype=u8)
+    for codes in (torch.zeros(1, 100, dtype=u8),                     # a row without the bytes behind it
+                  large[:100].view(1, 100),                          # those behind it are another's
+                  large[:17].view(1, 17),
+                  torch.as_strided(torch.zeros(49, dtype=u8), (2, 17), (32, 1)),     # the last row ends early
+                  torch.as_strided(torch.zeros(4095, dtype=u8), (3, 100), (112, 1), 4095 - 324),
+                  torch.zeros(3, 100, dtype=u8)):                    # rows side by side
+        with pytest.raises(lm.LionMuonError) as e:
+            make(codes)
+        assert e.value.status == BAD and "16 bytes" in str(e.value)
+    for rows, cols, codes in ((1, 100, torch.zeros(1, 112, dtype=u8)[:, :100]),
+                              (1, 17, large.view(16, 256)[3:4, :17]),
+                              (1, 128, large[:128].view(1, 128)),
+                              (2, 17, torch.as_strided(torch.zeros(64, dtype=u8), (2, 17), (32, 1))),
+                              (3, 100, torch.as_strided(torch.zeros(4096, dtype=u8), (3, 100), (112, 1), 4096 - 336)),
+                              (0, 100, torch.zeros(0, 100, dtype=u8)), (3, 0, torch.zeros(3, 0, dtype=u8))):
+        k = make(codes)
+        d = k._desc
+        assert k.shape == (rows, cols) and d.ld_codes >= -(-cols // 16) * 16
+        if rows and cols:
+            end = (rows - 1) * d.ld_codes + -(-cols // 16) * 16
+            assert codes.storage_offset() + end <= codes.untyped_storage().nbytes()
