@@ -94,14 +94,53 @@ class Checkpoint:
     operators write 0 behind the last code): ``codes`` are the first columns of a
     tensor with such rows."""
 
-    __slots__ = ("shape", "device", "_desc", "_buffer", "_codes", "_scales")
+    __slots__ = ("shape", "device", "_buffer", "_place", "_codes", "_scales")
 
     def __init__(self, codes, scales):
         for t, name in ((codes, "codes"), (scales, "scales")):
             if not isinstance(t, torch.Tensor):
                 raise TypeError(f"{name} must be a torch.Tensor")
+        self._buffer = None
+        self._codes = codes
+        self._scales = scales
+        self.shape = codes.shape
+        self.device = codes.device
+        self._desc          # (checked here, and again by each call)
+
+    @classmethod
+    def empty(cls, rows, cols, device="cuda"):
+        """An uninitialised checkpoint (filled by the operators that write one):
+        its codes and scales lie in one allocation."""
+        ld, blocks = -(-cols // 16) * 16, -(-cols // CHECKPOINT_BLOCK)
+        ld_scales = -(-blocks // 4) * 4
+        self = cls.__new__(cls)
+        self._buffer = buffer = torch.empty(rows * (ld + ld_scales), dtype=torch.uint8, device=device)
+        self.shape = torch.Size((rows, cols))
+        self.device = buffer.device
+        base = buffer.data_ptr()
+        self._place = lm_checkpoint(base, base + rows * ld if base else 0, rows, cols, ld,
+                                    ld_scales)
+        return self
+
+    @property
+    def _desc(self):
+        """The descriptor of a call: of the memory that the tensors have now."""
+        if self._buffer is None:
+            return self._described()
+        d = self._place
+        base = self._buffer.data_ptr()
+        if base != d.codes:
+            d = self._place = lm_checkpoint(base, base + d.rows * d.ld_codes if base else 0, d.rows,
+                                            d.cols, d.ld_codes, d.ld_scales)
+        return d
+
+    def _described(self):
+        codes, scales = self._codes, self._scales
+        for t, name in ((codes, "codes"), (scales, "scales")):
             if t.dtype != torch.uint8 or t.dim() != 2:
                 _invalid(f"{name} must be a 2-D uint8 tensor")
+        if codes.shape != self.shape or codes.device != self.device:
+            _invalid("codes have another shape or device than the checkpoint was made with")
         rows, cols = codes.shape
         blocks = -(-cols // CHECKPOINT_BLOCK)
         if scales.shape != (rows, blocks):
@@ -120,45 +159,23 @@ class Checkpoint:
         if rows > 1 and ld_scales % 4 == 0 and rows * ld_scales > \
                 scales.untyped_storage().nbytes() - scales.storage_offset():
             _invalid("the last row of scales must be as long as the others")
-        self.shape = codes.shape
-        self.device = codes.device
-        self._buffer = None
-        self._codes = codes
-        self._scales = scales
-        self._desc = lm_checkpoint(codes.data_ptr(), scales.data_ptr(), rows, cols,
-                                   ld if rows > 1 else whole,
-                                   ld_scales if rows > 1 else blocks)
-
-    @classmethod
-    def empty(cls, rows, cols, device="cuda"):
-        """An uninitialised checkpoint (filled by the operators that write one):
-        its codes and scales lie in one allocation."""
-        ld, blocks = -(-cols // 16) * 16, -(-cols // CHECKPOINT_BLOCK)
-        ld_scales = -(-blocks // 4) * 4
-        self = cls.__new__(cls)
-        self._buffer = buffer = torch.empty(rows * (ld + ld_scales), dtype=torch.uint8, device=device)
-        self.shape = torch.Size((rows, cols))
-        self.device = buffer.device
-        self._codes = self._scales = None
-        base = buffer.data_ptr()
-        self._desc = lm_checkpoint(base, base + rows * ld if base else 0, rows, cols, ld,
-                                   ld_scales)
-        return self
+        return lm_checkpoint(codes.data_ptr(), scales.data_ptr(), rows, cols,
+                             ld if rows > 1 else whole, ld_scales if rows > 1 else blocks)
 
     @property
     def codes(self):
-        if self._codes is None:
-            rows, ld = self._desc.rows, self._desc.ld_codes
-            self._codes = self._buffer[:rows * ld].view(rows, ld)[:, :self._desc.cols]
-        return self._codes
+        if self._buffer is None:
+            return self._codes
+        d = self._place
+        return self._buffer[:d.rows * d.ld_codes].view(d.rows, d.ld_codes)[:, :d.cols]
 
     @property
     def scales(self):
-        if self._scales is None:
-            rows, cols, d = self._desc.rows, self._desc.cols, self._desc
-            self._scales = self._buffer[rows * d.ld_codes:].view(rows, d.ld_scales)[
-                :, :-(-cols // CHECKPOINT_BLOCK)]
-        return self._scales
+        if self._buffer is None:
+            return self._scales
+        d = self._place
+        return self._buffer[d.rows * d.ld_codes:].view(d.rows, d.ld_scales)[
+            :, :-(-d.cols // CHECKPOINT_BLOCK)]
 
 
 # -- marshalling -------------------------------------------------------------

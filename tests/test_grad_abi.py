@@ -335,3 +335,43 @@ def test_checkpoint_with_codes_that_end_inside_16_bytes_is_refused():
         if rows and cols:
             end = (rows - 1) * d.ld_codes + -(-cols // 16) * 16
             assert codes.storage_offset() + end <= codes.untyped_storage().nbytes()
+
+
+def test_checkpoint_is_described_as_its_tensors_are_at_the_call():
+    """Tensors whose storage was exchanged (``set_``, ``.data``) or resized since the
+    checkpoint was made: the next call gets the new memory, or is refused."""
+    import torch
+    u8 = torch.uint8
+
+    def place(k):
+        return k._desc.codes, k._desc.scales
+
+    codes, scales = torch.zeros(3, 256, dtype=u8), torch.zeros(3, 2, dtype=u8)
+    k = gr.Checkpoint(codes, scales)
+    assert place(k) == (codes.data_ptr(), scales.data_ptr())
+    before, old = codes.data_ptr(), codes.untyped_storage()      # (kept: the new one lies elsewhere)
+    codes.set_(torch.zeros(3, 256, dtype=u8))
+    scales.data = torch.ones(3, 2, dtype=u8)
+    assert place(k) == (codes.data_ptr(), scales.data_ptr()) and codes.data_ptr() != before
+    assert k.codes is codes and old.data_ptr() == before
+    # another layout is read anew, another shape or type is not the checkpoint any more
+    codes.set_(torch.zeros(3, 512, dtype=u8)[:, :256])
+    assert k._desc.ld_codes == 512
+    for other in (torch.zeros(4, 256, dtype=u8), torch.zeros(3, 255, dtype=u8)):
+        codes.data = other
+        with pytest.raises(lm.LionMuonError):
+            k._desc
+    codes.data = torch.as_strided(torch.zeros(768, dtype=u8), (3, 256), (1, 3))
+    with pytest.raises(lm.LionMuonError):
+        k._desc
+    # storage given back and taken again, of tensors passed in and of an allocated one
+    codes, scales = torch.zeros(3, 240, dtype=u8), torch.zeros(3, 2, dtype=u8)
+    k, own = gr.Checkpoint(codes, scales), gr.Checkpoint.empty(5, 300, "cpu")
+    for c in (k, own):
+        storage = c.codes.untyped_storage()
+        size = storage.nbytes()
+        storage.resize_(0)
+        assert not c._desc.codes                       # refused by the entry points: null data
+        storage.resize_(size)
+        d = c._desc
+        assert d.codes == storage.data_ptr() == c.codes.data_ptr() and d.scales == c.scales.data_ptr()
