@@ -373,8 +373,9 @@ __global__ __launch_bounds__(kRowThreads) void activation_grad_kernel(BlockWalk 
         o[j] = silu * u[j];
       } else {
         const float p = gelu_gate<T>(x[j]);
-        // d/dx sigmoid(2 z) = 2 p (1 - p) z'
-        const float z = kGeluC * fmaf(3.0f * kGeluA * x[j], x[j], 1.0f);
+        // d/dx sigmoid(2 z) = 2 p (1 - p) z', z' at |x| <= 16: beyond 11 p is 0 or 1 and
+        // the term is 0, which x^2 would make NaN where it overflows
+        const float m = fminf(fabsf(x[j]), 16.0f), z = kGeluC * fmaf(3.0f * kGeluA * m, m, 1.0f);
         dx[j] = d[j] * fmaf(x[j] * p * (1.0f - p), 2.0f * z, p);
         o[j] = x[j] * p;
       }

@@ -658,3 +658,20 @@ def test_last_columns_of_widths_off_16_bytes_in_aligned_rows(rows, sizes, n, k, 
             want, mag = p @ q, p.abs() @ q.abs()
             err = (got.double() - want).abs()
             assert (err <= hs * 1.01 * want.abs() + sum_bound(p.shape[1]) * mag).all()
+
+
+def test_gelu_gradient_of_numbers_of_any_size():
+    """Where x^2 leaves the type's range the slope is 1 or 0, as from |x| = 16 on; up to
+    there the border of the two forms is not seen."""
+    for name, dt in TYPES.items():
+        top = torch.finfo(dt).max
+        v = [m for m in (15.9, 16.0, 16.1, 1e3, 6e4, 1e10, 1e19, 2e19, 1e20, 1e30, top) if m <= top]
+        x = torch.tensor([v + [-m for m in v]], dtype=torch.float64).to(dt).cuda()
+        da, h = gr.lionmuon_activation_grad(torch.ones_like(x), x, "gelu", recompute=True)
+        assert (f64(da)[0, :len(v)] == 1).all() and (f64(da)[0, len(v):] == 0).all(), name
+        assert (f64(h)[0, :len(v)] == f64(x)[0, :len(v)]).all() and (f64(h)[0, len(v):] == 0).all(), name
+        # from a checkpoint, whose values these are (one in each block)
+        kept = gr.lionmuon_checkpoint(torch.full((1, 128), 2.0 ** 15 if dt == torch.float16 else 2.0 ** 100, dtype=dt, device="cuda"))
+        assert (gr.lionmuon_activation_grad(torch.ones(1, 128, dtype=dt, device="cuda"), kept, "gelu")[0] == 1).all()
+        nan = torch.full((1, 3), float("nan"), dtype=dt, device="cuda")
+        assert gr.lionmuon_activation_grad(torch.ones_like(nan), nan, "gelu")[0].isnan().all()
