@@ -21,7 +21,8 @@
  * one byte e + 127 for each LM_CHECKPOINT_BLOCK columns of a row. A block's e
  * is the smallest integer >= -100 with max|x| <= 448 * 2^e over its finite
  * values; code = e4m3(x * 2^-e), to nearest, ties to even; NaN and infinities
- * become NaN. A code stands for code * 2^e, which bf16 holds exactly. Each
+ * become NaN. A code stands for code * 2^e, which bf16 holds exactly (where e is
+ * 120, its largest, codes go to 240 only, so that what they stand for is finite). Each
  * value of magnitude above 2^-6 * 2^e is off by at most 2^-4 of itself, a
  * smaller one by 2^-10 * 2^e. Rows of codes start 16-byte aligned (codes pointer
  * and ld_codes multiples of 16, ld_codes >= cols); the bytes between cols and

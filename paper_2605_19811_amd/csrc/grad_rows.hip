@@ -97,6 +97,8 @@ __device__ __forceinline__ bool is_finite(float v) {
   return (__builtin_bit_cast(uint32_t, v) & 0x7f800000u) != 0x7f800000u;
 }
 
+constexpr int kTopExponent = 120;      // e of the largest fp32 numbers
+
 // Codes of one block of 128 columns, eight a lane; all 16 lanes enter. Returns the
 // scale byte. 448 = 1.75 * 2^8 is e4m3's largest value: with max|x| = m 2^k,
 // 1 <= m < 2, the least e with max|x| <= 448 * 2^e is k - 8, or k - 7 for
@@ -112,6 +114,12 @@ __device__ __forceinline__ uint32_t encode8(const float v[8], u32x2* codes) {
   float s[8];
 #pragma unroll
   for (int j = 0; j < 8; ++j) s[j] = is_finite(v[j]) ? v[j] * inv : __builtin_nanf("");
+  if (e == kTopExponent) {
+    // 256 * 2^120 would be infinite: the largest code stands for 240 * 2^120, within 2^-4
+    // of every value above it
+#pragma unroll
+    for (int j = 0; j < 8; ++j) s[j] = fabsf(s[j]) > 240.0f ? copysignf(240.0f, s[j]) : s[j];
+  }
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
     int c = __builtin_amdgcn_cvt_pk_fp8_f32(s[4 * h], s[4 * h + 1], 0, false);

@@ -675,3 +675,26 @@ def test_gelu_gradient_of_numbers_of_any_size():
         assert (gr.lionmuon_activation_grad(torch.ones(1, 128, dtype=dt, device="cuda"), kept, "gelu")[0] == 1).all()
         nan = torch.full((1, 3), float("nan"), dtype=dt, device="cuda")
         assert gr.lionmuon_activation_grad(torch.ones_like(nan), nan, "gelu")[0].isnan().all()
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+def test_checkpoint_of_the_largest_numbers_is_finite(dtype):
+    """Above 1.9375 * 2^127 the nearest code of a block with e = 120 would stand for 2^128."""
+    dt = TYPES[dtype]
+    top = torch.finfo(dt).max
+    v = torch.tensor([top, -top, 1.9375 * 2.0 ** 127, -1.9453125 * 2.0 ** 127, 1.875 * 2.0 ** 127, 1.75 * 2.0 ** 127,
+                      -1.7578125 * 2.0 ** 127, 2.0 ** 127, 3e37, -1.0, 0.0], dtype=torch.float64)
+    x = torch.full((3, 200), 0.5, dtype=dt, device="cuda")
+    x[0, 5:5 + len(v)] = v.to(dt).cuda()
+    x[1, 140] = top
+    x[2, 0], x[2, 1] = top, float("nan")
+    for k in (gr.lionmuon_checkpoint(x), gr.lionmuon_activation(x, "gelu", checkpoint=True)[1]):
+        e = f64(k.scales).astype(int) - 127
+        assert (e == ref.block_exponents(f64(x))).all() and e.max() == 120
+        for t in (torch.float32, torch.bfloat16):
+            got, want = f64(gr.lionmuon_checkpoint_restore(k, t)), f64(x)
+            assert np.isnan(got[2, 1])
+            got[2, 1] = want[2, 1] = 0.0
+            scale = np.ldexp(1.0, np.repeat(e, 128, axis=1)[:, :200])
+            assert (np.abs(got - want) <= 2.0 ** -4 * np.abs(want) * (np.abs(want) >= 2.0 ** -6 * scale) + 2.0 ** -10 * scale).all()
+            assert (np.abs(got) <= 240 * 2.0 ** 120).all() and got[0, 5] == -got[0, 6] == 240 * 2.0 ** 120
