@@ -12,8 +12,9 @@
 Argument marshalling only, as in ``lionmuon.py``: matrices are 2-D GPU tensors
 whose rows are contiguous (they may lie apart), calls are asynchronous on
 ``stream`` (default: the current stream of the tensors' device), outputs that
-are not passed in are allocated by torch. Autograd sees none of it. There is
-no fallback.
+are not passed in are allocated by torch. Autograd records none of it; tensors that
+are passed in and written count as changed in place, so that a backward pass which
+needs what they held before fails. There is no fallback.
 """
 from __future__ import annotations
 
@@ -133,6 +134,10 @@ class Checkpoint:
             d = self._place = lm_checkpoint(base, base + d.rows * d.ld_codes if base else 0, d.rows,
                                             d.cols, d.ld_codes, d.ld_scales)
         return d
+
+    def _written(self):
+        for t in (self._codes, self._scales) if self._buffer is None else (self._buffer,):
+            _written(t)
 
     def _described(self):
         codes, scales = self._codes, self._scales
@@ -300,6 +305,9 @@ def _done(status, what):
         _check(status, what)
 
 
+_written = torch.autograd.graph.increment_version      # of a tensor that was passed in
+
+
 # -- checkpoints -------------------------------------------------------------
 def lionmuon_checkpoint(x, out: Checkpoint | None = None, stream=None) -> Checkpoint:
     """8-bit checkpoint of a 2-D float32, bfloat16 or float16 tensor."""
@@ -309,10 +317,11 @@ def lionmuon_checkpoint(x, out: Checkpoint | None = None, stream=None) -> Checkp
         with _switched(device, stream):
             return lionmuon_checkpoint(x, out)
     m = _matrix(x, "x", device)
-    if out is None:
-        out = Checkpoint.empty(m.rows, m.cols, device)
-    _done(_lib().lionmuon_checkpoint(m, _codes(out, "out", device), handle), "lionmuon_checkpoint")
-    return out
+    kept = Checkpoint.empty(m.rows, m.cols, device) if out is None else out
+    _done(_lib().lionmuon_checkpoint(m, _codes(kept, "out", device), handle), "lionmuon_checkpoint")
+    if out is not None:
+        out._written()
+    return kept
 
 
 def lionmuon_checkpoint_restore(checkpoint: Checkpoint, dtype=torch.bfloat16, out=None,
@@ -327,11 +336,12 @@ def lionmuon_checkpoint_restore(checkpoint: Checkpoint, dtype=torch.bfloat16, ou
     if handle is None:
         with _switched(device, stream):
             return lionmuon_checkpoint_restore(checkpoint, dtype, out)
-    if out is None:
-        out = torch.empty(checkpoint.shape, dtype=dtype, device=device)
-    _done(_lib().lionmuon_checkpoint_restore(checkpoint._desc, _matrix(out, "out", device), handle),
+    x = torch.empty(checkpoint.shape, dtype=dtype, device=device) if out is None else out
+    _done(_lib().lionmuon_checkpoint_restore(checkpoint._desc, _matrix(x, "out", device), handle),
           "lionmuon_checkpoint_restore")
-    return out
+    if out is not None:
+        _written(out)
+    return x
 
 
 # -- activation functions ----------------------------------------------------
@@ -357,13 +367,17 @@ def lionmuon_activation(a, kind, out=None, checkpoint=False, stream=None):
     if code == 1 and cols % 2:
         _invalid("a must have an even number of columns")
     if out is None:
-        out, mo = _new(rows, cols // (1 + code), a, m.dtype)
+        h, mh = _new(rows, cols // (1 + code), a, m.dtype)
     else:
-        mo = _matrix(out, "out", device)
+        h, mh = out, _matrix(out, "out", device)
     kept = _wanted(checkpoint, rows, cols, device)
-    _done(_lib().lionmuon_activation(m, code, mo, None if kept is None else kept._desc, handle),
+    _done(_lib().lionmuon_activation(m, code, mh, None if kept is None else kept._desc, handle),
           "lionmuon_activation")
-    return out, kept
+    if out is not None:
+        _written(out)
+    if kept is checkpoint and kept is not None:
+        kept._written()
+    return h, kept
 
 
 def lionmuon_activation_grad(dh, a, kind, out=None, recompute=False, stream=None):
@@ -384,18 +398,22 @@ def lionmuon_activation_grad(dh, a, kind, out=None, recompute=False, stream=None
     else:
         ma = _matrix(a, "a", device)
     if out is None:
-        out, mo = _new(rows, cols * (1 + code), dh, m.dtype)
+        da, mda = _new(rows, cols * (1 + code), dh, m.dtype)
     else:
-        mo = _matrix(out, "out", device)
+        da, mda = out, _matrix(out, "out", device)
     if isinstance(recompute, torch.Tensor):
         h, mh = recompute, _matrix(recompute, "recompute", device)
     elif recompute:
         h, mh = _new(rows, cols, dh, m.dtype)
     else:
         h = mh = None
-    _done(_lib().lionmuon_activation_grad(m, ma, mk, code, mo, mh, handle),
+    _done(_lib().lionmuon_activation_grad(m, ma, mk, code, mda, mh, handle),
           "lionmuon_activation_grad")
-    return out, h
+    if out is not None:
+        _written(out)
+    if h is recompute and h is not None:
+        _written(h)
+    return da, h
 
 
 # -- root-mean-square norm ---------------------------------------------------
@@ -435,6 +453,12 @@ def lionmuon_rmsnorm(x, weight, residual=None, eps=1e-5, out=None, sum_out=None,
     _done(_lib().lionmuon_rmsnorm(m, mr, w, eps, my, ms, rstd.data_ptr(),
                                   None if kept is None else kept._desc, handle),
           "lionmuon_rmsnorm")
+    if out is not None and y is not None:
+        _written(y)
+    if sum_out is not None:
+        _written(sum_out)
+    if kept is checkpoint and kept is not None:
+        kept._written()
     return y, s, rstd, kept
 
 
@@ -483,6 +507,10 @@ def lionmuon_rmsnorm_grad(dy, s, weight, rstd, residual_grad=None, out=None, wei
     _done(_lib().lionmuon_rmsnorm_grad(m, ms, mk, w, r, mr, mdx, pw, 1 if accumulate else 0,
                                        None if ws is None else ws.data_ptr(), nbytes, handle),
           "lionmuon_rmsnorm_grad")
+    if out is not None and dx is not None:
+        _written(dx)
+    if weight_grad is not None and dw is not None:
+        _written(dw)
     return dx, dw
 
 
@@ -508,11 +536,13 @@ def lionmuon_grouped_product(x, w, offsets, out=None, stream=None):
     mw = _stack(w, "w", device)
     at = _offsets(offsets, mw.count, device)
     if out is None:
-        out, mo = _new(m.rows, mw.rows, x, m.dtype)
+        y, mo = _new(m.rows, mw.rows, x, m.dtype)
     else:
-        mo = _matrix(out, "out", device)
+        y, mo = out, _matrix(out, "out", device)
     _done(_lib().lionmuon_grouped_product(m, mw, at, mo, handle), "lionmuon_grouped_product")
-    return out
+    if out is not None:
+        _written(out)
+    return y
 
 
 def lionmuon_grouped_input_grad(dy, w, offsets, out=None, stream=None):
@@ -526,11 +556,13 @@ def lionmuon_grouped_input_grad(dy, w, offsets, out=None, stream=None):
     mw = _stack(w, "w", device)
     at = _offsets(offsets, mw.count, device)
     if out is None:
-        out, mo = _new(m.rows, mw.cols, dy, m.dtype)
+        dx, mo = _new(m.rows, mw.cols, dy, m.dtype)
     else:
-        mo = _matrix(out, "out", device)
+        dx, mo = out, _matrix(out, "out", device)
     _done(_lib().lionmuon_grouped_input_grad(m, mw, at, mo, handle), "lionmuon_grouped_input_grad")
-    return out
+    if out is not None:
+        _written(out)
+    return dx
 
 
 def lionmuon_grouped_weight_grad(dy, x, offsets, out=None, accumulate=False, stream=None):
@@ -556,11 +588,10 @@ def lionmuon_grouped_weight_grad(dy, x, offsets, out=None, accumulate=False, str
         _check_place(offsets, "offsets", device)
         experts = offsets.numel() - 1
         at = _offsets(offsets, experts, device)
-        out = torch.empty((experts, m.cols, cols), dtype=torch.float32, device=device)
+        dw = torch.empty((experts, m.cols, cols), dtype=torch.float32, device=device)
+        mo = _stack(dw, "out", device)
     else:
-        experts = None
-    mo = _stack(out, "out", device)
-    if experts is None:
+        dw, mo = out, _stack(out, "out", device)
         experts = mo.count
         at = _offsets(offsets, experts, device)
     nbytes = lionmuon_grouped_workspace_bytes(m.rows, experts, m.cols, cols)
@@ -568,7 +599,9 @@ def lionmuon_grouped_weight_grad(dy, x, offsets, out=None, accumulate=False, str
     _done(_lib().lionmuon_grouped_weight_grad(m, mx, mk, at, mo, 1 if accumulate else 0,
                                               None if ws is None else ws.data_ptr(), nbytes,
                                               handle), "lionmuon_grouped_weight_grad")
-    return out
+    if out is not None:
+        _written(out)
+    return dw
 
 
 def lionmuon_grouped_workspace_bytes(rows, experts, n, k) -> int:

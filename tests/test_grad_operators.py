@@ -698,3 +698,57 @@ def test_checkpoint_of_the_largest_numbers_is_finite(dtype):
             scale = np.ldexp(1.0, np.repeat(e, 128, axis=1)[:, :200])
             assert (np.abs(got - want) <= 2.0 ** -4 * np.abs(want) * (np.abs(want) >= 2.0 ** -6 * scale) + 2.0 ** -10 * scale).all()
             assert (np.abs(got) <= 240 * 2.0 ** 120).all() and got[0, 5] == -got[0, 6] == 240 * 2.0 ** 120
+
+
+# -- tensors that are passed in and written -----------------------------------
+def test_tensors_that_are_written_count_as_changed():
+    """Every output that is passed in, so that autograd notices a saved tensor that a
+    call has overwritten; inputs do not count."""
+    dt = torch.bfloat16
+    x, r, dy = (make((6, 256), dt, s) for s in (1, 2, 3))
+    w = torch.rand(256, device="cuda")
+    at = torch.tensor([0, 2, 6], dtype=torch.int32, device="cuda")
+    stack = torch.randn(2, 64, 256, device="cuda").to(dt)
+    rstd = gr.lionmuon_rmsnorm(x, w)[2]
+
+    def new(*shape, t=dt):
+        return torch.zeros(*shape, dtype=t, device="cuda")
+
+    def kept():
+        return gr.Checkpoint(new(6, 256, t=torch.uint8), new(6, 2, t=torch.uint8))
+
+    def versions(ts):
+        return [t._version for t in ts]
+
+    inputs = [x, r, dy, w, at, stack, rstd]
+    k, dout = gr.lionmuon_checkpoint(x), new(6, 64)
+    for call, outputs in (
+            (lambda a: gr.lionmuon_checkpoint_restore(k, out=a), [new(6, 256)]),
+            (lambda a: gr.lionmuon_activation(x, "gelu", out=a), [new(6, 256)]),
+            (lambda a, b: gr.lionmuon_activation_grad(dy, k, "gelu", out=a, recompute=b), [new(6, 256), new(6, 256)]),
+            (lambda a, b: gr.lionmuon_rmsnorm(x, w, residual=r, out=a, sum_out=b), [new(6, 256), new(6, 256)]),
+            (lambda a, b: gr.lionmuon_rmsnorm_grad(dy, k, w, rstd, out=a, weight_grad=b), [new(6, 256), new(256, t=torch.float32)]),
+            (lambda a: gr.lionmuon_grouped_product(x, stack, at, out=a), [new(6, 64)]),
+            (lambda a: gr.lionmuon_grouped_input_grad(dout, stack, at, out=a), [new(6, 256)]),
+            (lambda a: gr.lionmuon_grouped_weight_grad(dout, k, at, out=a), [new(2, 64, 256, t=torch.float32)])):
+        before, held = versions(outputs), versions(inputs)
+        call(*outputs)
+        assert all(v > b for v, b in zip(versions(outputs), before))
+        assert versions(inputs) == held
+    for write in (lambda c: gr.lionmuon_checkpoint(x, out=c), lambda c: gr.lionmuon_activation(x, "gelu", checkpoint=c),
+                  lambda c: gr.lionmuon_rmsnorm(x, w, checkpoint=c)):
+        for c in (kept(), gr.Checkpoint.empty(6, 256)):
+            codes, scales = c.codes, c.scales
+            before = versions([codes, scales])
+            write(c)
+            assert all(v > b for v, b in zip(versions([codes, scales]), before))
+    # a backward pass that needs the residual as it was
+    p = torch.ones(6, 256, device="cuda", requires_grad=True)
+    stream = r.float()
+    loss = (p * stream).sum()
+    gr.lionmuon_rmsnorm(x.float(), w, residual=stream, sum_out=stream)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        loss.backward()
+    with torch.inference_mode():
+        out = new(6, 256)
+        assert gr.lionmuon_rmsnorm(x, w, out=out)[0] is out and (out != 0).any()
