@@ -586,6 +586,8 @@ def lionmuon_grouped_weight_grad(dy, x, offsets, out=None, accumulate=False, str
         if accumulate:
             _invalid("accumulate needs out")
         _check_place(offsets, "offsets", device)
+        if offsets.numel() < 2:
+            _invalid("offsets must hold at least two values")
         experts = offsets.numel() - 1
         at = _offsets(offsets, experts, device)
         dw = torch.empty((experts, m.cols, cols), dtype=torch.float32, device=device)

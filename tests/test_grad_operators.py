@@ -752,3 +752,17 @@ def test_tensors_that_are_written_count_as_changed():
     with torch.inference_mode():
         out = new(6, 256)
         assert gr.lionmuon_rmsnorm(x, w, out=out)[0] is out and (out != 0).any()
+
+
+def test_offsets_of_no_expert_are_refused():
+    x, dy = make((6, 64), torch.bfloat16, 1), make((6, 32), torch.bfloat16, 2)
+    for n in (0, 1):
+        offsets = torch.zeros(n, dtype=torch.int32, device="cuda")
+        out = torch.zeros(max(n - 1, 0), 32, 64, device="cuda")
+        for call in (lambda: gr.lionmuon_grouped_weight_grad(dy, x, offsets),
+                     lambda: gr.lionmuon_grouped_weight_grad(dy, x, offsets, out=out),
+                     lambda: gr.lionmuon_grouped_product(x, out.bfloat16(), offsets),
+                     lambda: gr.lionmuon_grouped_input_grad(dy, out.bfloat16(), offsets)):
+            with pytest.raises(lm.LionMuonError) as e:
+                call()
+            assert e.value.status == lm.LM_ERR_INVALID_ARGUMENT
