@@ -8,6 +8,8 @@
 #include <cstddef>
 #include <cstdint>
 
+#include "grad_plan.h"
+
 namespace lm {
 
 enum class Elem : int32_t { kF32 = 0, kBF16 = 1, kF16 = 2 };
@@ -26,9 +28,6 @@ struct CkptView {
 };
 
 constexpr int kCkptBlock = 128;
-
-// Workgroups of a launch at most: with 512 threads each, 2^31 threads.
-constexpr int64_t kMaxWorkgroups = int64_t(1) << 22;
 
 hipError_t launch_checkpoint(Elem t, MatView x, CkptView out, int64_t rows, int64_t cols,
                              hipStream_t stream);
