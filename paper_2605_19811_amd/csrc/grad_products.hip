@@ -203,11 +203,12 @@ template <int MODE, int W, int KS>
 struct Stage {
   static constexpr int kChunks = W * KS / 8;                        // of 16 bytes
   static constexpr int kPerRow = MODE == kRows ? KS / 8 : W / 8;    // chunks of an LDS row
+  static_assert(MODE != kRows || kPerRow == 8, "stages of 64 values");
   // Physical chunk of logical chunk c in LDS row r is c ^ swz(r): 16 rows of a
   // fragment read (kRows), or the four rows of a transpose read (kCols), fall into
   // different banks. (Rows of 64 columns are 8 chunks: there rows go in pairs.)
   __device__ static __forceinline__ int swz(int r) {
-    if (MODE == kRows) return kPerRow == 4 ? (r >> 2) & 3 : (r & 7) ^ ((r >> 3) & 1);
+    if (MODE == kRows) return (r & 7) ^ ((r >> 3) & 1);
     return kPerRow == 8 ? ((r >> 1) & 1) * 4 : (r & 3) * 4;
   }
   __device__ static __forceinline__ void place(int c, int* row, int* chunk) {
