@@ -247,13 +247,13 @@ def _codes(c, name, device):
 
 
 def _wanted(checkpoint, rows, cols, device):
-    """The Checkpoint to write: None, a new one, or the one passed in."""
+    """The Checkpoint to write and its descriptor: None, a new one, or the one passed in."""
     if checkpoint is False or checkpoint is None:
-        return None
+        return None, None
     if isinstance(checkpoint, Checkpoint):
-        _codes(checkpoint, "checkpoint", device)
-        return checkpoint
-    return Checkpoint.empty(rows, cols, device)
+        return checkpoint, _codes(checkpoint, "checkpoint", device)
+    new = Checkpoint.empty(rows, cols, device)
+    return new, new._place
 
 
 def _vector(t, n, name, device):
@@ -317,11 +317,13 @@ def lionmuon_checkpoint(x, out: Checkpoint | None = None, stream=None) -> Checkp
         with _switched(device, stream):
             return lionmuon_checkpoint(x, out)
     m = _matrix(x, "x", device)
-    kept = Checkpoint.empty(m.rows, m.cols, device) if out is None else out
-    _done(_lib().lionmuon_checkpoint(m, _codes(kept, "out", device), handle), "lionmuon_checkpoint")
-    if out is not None:
-        out._written()
-    return kept
+    if out is None:
+        kept = Checkpoint.empty(m.rows, m.cols, device)
+        _done(_lib().lionmuon_checkpoint(m, kept._place, handle), "lionmuon_checkpoint")
+        return kept
+    _done(_lib().lionmuon_checkpoint(m, _codes(out, "out", device), handle), "lionmuon_checkpoint")
+    out._written()
+    return out
 
 
 def lionmuon_checkpoint_restore(checkpoint: Checkpoint, dtype=torch.bfloat16, out=None,
@@ -370,9 +372,8 @@ def lionmuon_activation(a, kind, out=None, checkpoint=False, stream=None):
         h, mh = _new(rows, cols // (1 + code), a, m.dtype)
     else:
         h, mh = out, _matrix(out, "out", device)
-    kept = _wanted(checkpoint, rows, cols, device)
-    _done(_lib().lionmuon_activation(m, code, mh, None if kept is None else kept._desc, handle),
-          "lionmuon_activation")
+    kept, mk = _wanted(checkpoint, rows, cols, device)
+    _done(_lib().lionmuon_activation(m, code, mh, mk, handle), "lionmuon_activation")
     if out is not None:
         _written(out)
     if kept is checkpoint and kept is not None:
@@ -449,9 +450,8 @@ def lionmuon_rmsnorm(x, weight, residual=None, eps=1e-5, out=None, sum_out=None,
     else:
         y, my = out, _matrix(out, "out", device)
     rstd = weight.new_empty(rows)
-    kept = _wanted(checkpoint, rows, cols, device)
-    _done(_lib().lionmuon_rmsnorm(m, mr, w, eps, my, ms, rstd.data_ptr(),
-                                  None if kept is None else kept._desc, handle),
+    kept, mk = _wanted(checkpoint, rows, cols, device)
+    _done(_lib().lionmuon_rmsnorm(m, mr, w, eps, my, ms, rstd.data_ptr(), mk, handle),
           "lionmuon_rmsnorm")
     if out is not None and y is not None:
         _written(y)
