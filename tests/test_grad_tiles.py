@@ -149,3 +149,31 @@ def test_weight_gradients_by_every_tile(rows, experts, n, k, tile, cut, off, dty
         for e in range(experts):
             a, b = dy[at[e]:at[e + 1]].double(), v[at[e]:at[e + 1]].double()
             assert right(dw[e], a.t(), b, 0.0), (coded, e)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("rows,width,depth", [(64, 64, 131072), (300, 1100, 32768), (2500, 2056, 16384)])
+def test_long_contractions_of_one_sign(rows, width, depth, dtype):
+    """The sums of a long contraction do not drift: the matrix unit adds 16 products at a
+    time and rounds to nearest, so that depth / 16 independent errors of 2^-24 of a
+    partial sum at most stay below eight times their root (the number of results is
+    below 2^23). One-sided errors would reach depth / 32 * 2^-24, two to six times
+    that, beside half a step of the result."""
+    dt = TYPES[dtype]
+    g = torch.Generator(device="cuda").manual_seed(depth)
+    x = (torch.rand(rows, depth, generator=g, device="cuda") * 0.5 + 0.5).to(dt)
+    w = ((torch.rand(1, width, depth, generator=g, device="cuda") * 0.5 + 0.5) * 2.0 ** -6).to(dt)
+    offsets = torch.tensor([0, rows], dtype=torch.int32, device="cuda")
+    want = torch.zeros(rows, width, dtype=torch.float64, device="cuda")
+    for c in range(0, depth, 8192):
+        want += x[:, c:c + 8192].double() @ w[0, :, c:c + 8192].double().t()
+    drift = 8 * 2.0 ** -24 * (depth / 16) ** 0.5
+    across = w.transpose(1, 2).contiguous()
+    for got in (gr.lionmuon_grouped_product(x, w, offsets), gr.lionmuon_grouped_input_grad(x, across, offsets)):
+        assert ((got.double() - want).abs() <= (torch.finfo(dt).eps / 2 + drift) * want).all()
+    # fp32 results are folded every 512: eight times the root of that, and as much for the folds
+    dy, xt = w[0].t().contiguous(), x.t().contiguous()
+    dw = gr.lionmuon_grouped_weight_grad(dy, xt, torch.tensor([0, depth], dtype=torch.int32, device="cuda"))[0]
+    folds = 8 * 2.0 ** -24 * (32 ** 0.5 + (depth / 512) ** 0.5)
+    assert ((dw.double() - want.t()).abs() <= folds * want.t()).all()
