@@ -9,9 +9,11 @@
 // values (128 bytes, eight 16-byte chunks XOR-swizzled by row); one that runs across
 // it as 64 rows of the tile's width, read through gfx950's LDS transpose reads, so
 // that no operand is ever transposed in memory. 256 x 256 tiles take 8192^3 at
-// 1340 TFLOP/s and 4096^3 at 1250 (the library's product: 1590, 1510): their 64 KB
-// of operands a stage, copied in 1 KB pieces, bound them (without copies 1340 -> 1470,
-// the matrix unit's own rate under the power limit). What it took, each
+// 1340 TFLOP/s and 4096^3 at 1280 (the library's product: 1670, 1560): their 64 KB
+// of operands a stage, copied in 1 KB pieces, bound them (without copies 1340 -> 1470;
+// the matrix unit is busy 0.60 to 0.66 of the time). The row products of these tiles
+// spill 6 (B by rows), 13 (B by columns) and 9 registers (both operands through
+// registers), all of them outside the loop over stages. What it took, each
 // measured on the kernel before: all stages' fragments read a step ahead and one
 // barrier a stage (853 -> 1104 at 8192^3), tiles counted on the device (an XCD with
 // two tiles more than CUs made every product take a round more: 4096^3 200 -> 110 us),
@@ -26,7 +28,7 @@
 // Ragged edges cost no branch in the loop: operands are read by buffer loads
 // whose descriptor ends at the last valid row, so what lies beyond reads as zero,
 // and lanes beyond the end of the contraction get an address outside. Operands off
-// 16 bytes go through registers instead (4096^3 with rows of odd length: 147 us).
+// 16 bytes go through registers instead (4096^3 with rows of 4097: Y 145 us, dX 173).
 #include <algorithm>
 #include <type_traits>
 
@@ -166,9 +168,10 @@ __device__ __forceinline__ int by_xcd(int bid, int chunk) {
   return (j / chunk * 8 + x) * chunk + j % chunk;
 }
 
-// The nth longest expert (the nth in order where there are too many to sort on
-// the way): workgroups start in this order, so that no long one starts last.
-// Selected bit by bit from the top, of equal ones in order.
+// The nth longest expert: workgroups start in this order, so that no long one starts
+// last. Selected bit by bit from the top, of equal ones in order. More experts than
+// the 64 lanes that hold one each start in order: their output then takes most of the
+// time (16384 x 4096 x 1024 by 128 skewed ones: 459 us for 2.1 GB).
 __device__ __forceinline__ int nth_longest(const int32_t* offsets, int experts, int rows, int n) {
   if (experts == 1 || experts > 64) return n;
   const int lane = threadIdx.x & 63, i = min(lane, experts - 1);
@@ -460,9 +463,11 @@ struct Tile {
   }
 
   // The K loop: out = sum over the contraction. FOLD > 0: after that many
-  // stages the accumulators are added to `out` and start again from zero (the
-  // matrix unit truncates where it adds to an accumulator, which long chains show;
-  // vector additions round).
+  // stages the accumulators are added to `out` and start again from zero. (The matrix
+  // unit rounds to nearest where it adds to an accumulator, so that the error grows
+  // with the root of the chain's length: for terms of one sign 1.0e-7 of the result
+  // after 512, 9.5e-7 after 32768, 1.9e-6 after 131072. fp32 results show that, folded
+  // ones stay at 1e-7 to 3e-7; 16-bit results, off by 2^-12 at least, do not.)
   //
   // A stage is kSteps steps of 16 SUB values. The fragments of a step are read while
   // the step before is multiplied, across stages too: one barrier a stage, before its
@@ -965,8 +970,9 @@ __device__ __forceinline__ int partial_slot(int first, int part) { return int(2 
 
 // 256 x 128 at most: the second set of sums (FOLD) takes as many registers as the
 // first. Eight waves of 64 x 64 read 128 KB of LDS a stage and copy 48 KB into it, about
-// 1400 of its 2000 cycles; that and the power limit bound it (8192^3: 1080 TFLOP/s; 32768 x
+// 1400 of its 2000 cycles, which bounds it (8192^3: 1080 TFLOP/s; 32768 x
 // 1280 x 5120: 450 us). From a checkpoint the codes' way through LDS adds 32 KB (515 us).
+// (128 x 128 with both operands through registers spills 4 of them.)
 // Experts one after the other instead of the longest first: 16384 x 4096 x 1024 by eight
 // skewed ones twice as long.
 template <typename T, int MB, class S, bool DA, bool DB>

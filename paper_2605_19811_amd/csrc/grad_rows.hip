@@ -5,8 +5,8 @@
 // A lane takes eight elements; the 16 lanes of a DPP row are the 128 columns that
 // share a scale, so a checkpoint's maximum is four lane rotations away, without
 // LDS, and every kernel that has a tensor in registers can store its checkpoint
-// on the way. 32768 x 4096 in bf16: checkpoint 5.3 TB/s, restore 6.9, norm 5.2, its
-// gradient 5.4, activations and their gradients 5.4 to 5.9 (a large copy: 5.15 to 5.5).
+// on the way. 32768 x 4096 in bf16: checkpoint 5.3 TB/s, restore 6.9, norm 5.1, its
+// gradient 5.4, activations and their gradients 5.4 to 5.9 (a large copy: 5.0 to 5.5).
 #include <type_traits>
 
 #include "grad_device.h"
@@ -156,8 +156,9 @@ struct BlockWalk {
   int32_t blocks, per;      // blocks of a row, rows of a workgroup
 };
 
-// Rows of a workgroup: four blocks for each of its groups of lanes, or one where
-// the whole tensor would not fill the chip otherwise.
+// Rows of a workgroup, whole ones: four blocks for each of its groups of lanes, or one
+// where the whole tensor would not fill the chip otherwise. A row of more blocks is one
+// workgroup's all the same, so that few rows of many columns leave CUs idle.
 BlockWalk walk_of(int64_t rows, int64_t cols) {
   BlockWalk w;
   w.rows = rows;
@@ -493,7 +494,8 @@ __global__ __launch_bounds__(team_threads<NT>()) void rmsnorm_kernel(NormArgs a)
 }
 
 // dx of each row; dweight summed over the rows of a workgroup in registers (the
-// four waves of a workgroup meet in LDS), one row of partials a workgroup.
+// four waves of a workgroup meet in LDS), one row of partials a workgroup. (fp32 rows
+// of more than 8192 columns from a checkpoint spill 8 registers.)
 template <typename T, int NT, int C, bool KEPT>
 __global__ __launch_bounds__(team_threads<NT>()) void rmsnorm_grad_kernel(NormArgs a) {
   constexpr int kTeams = team_threads<NT>() / NT;
