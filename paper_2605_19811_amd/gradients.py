@@ -95,18 +95,15 @@ class Checkpoint:
     operators write 0 behind the last code): ``codes`` are the first columns of a
     tensor with such rows."""
 
-    __slots__ = ("shape", "device", "_buffer", "_place", "_codes", "_scales")
+    __slots__ = ("shape", "device", "_buffer", "_place", "_codes", "_scales", "_layout")
 
     def __init__(self, codes, scales):
-        for t, name in ((codes, "codes"), (scales, "scales")):
-            if not isinstance(t, torch.Tensor):
-                raise TypeError(f"{name} must be a torch.Tensor")
-        self._buffer = None
+        if not isinstance(codes, torch.Tensor) or not isinstance(scales, torch.Tensor):
+            raise TypeError("codes and scales must be torch.Tensors")
+        self._buffer = self.shape = self.device = None
         self._codes = codes
         self._scales = scales
-        self.shape = codes.shape
-        self.device = codes.device
-        self._desc          # (checked here, and again by each call)
+        self._described()
 
     @classmethod
     def empty(cls, rows, cols, device="cuda"):
@@ -127,7 +124,10 @@ class Checkpoint:
     def _desc(self):
         """The descriptor of a call: of the memory that the tensors have now."""
         if self._buffer is None:
-            return self._described()
+            c, s = self._codes, self._scales
+            if (c.data_ptr(), s.data_ptr(), c.shape, c.stride(), s.stride()) != self._layout:
+                self._described()          # (all that the descriptor is made of)
+            return self._place
         d = self._place
         base = self._buffer.data_ptr()
         if base != d.codes:
@@ -140,20 +140,25 @@ class Checkpoint:
             _written(t)
 
     def _described(self):
+        """Checks the tensors and describes them as they are now."""
         codes, scales = self._codes, self._scales
-        for t, name in ((codes, "codes"), (scales, "scales")):
+        for t in (codes, scales):
             if t.dtype != torch.uint8 or t.dim() != 2:
-                _invalid(f"{name} must be a 2-D uint8 tensor")
-        if codes.shape != self.shape or codes.device != self.device:
+                _invalid(f"{'codes' if t is codes else 'scales'} must be a 2-D uint8 tensor")
+        shape, device = codes.shape, codes.device
+        if self.shape is None:
+            self.shape, self.device = shape, device
+        elif shape != self.shape or device != self.device:
             _invalid("codes have another shape or device than the checkpoint was made with")
-        rows, cols = codes.shape
+        rows, cols = shape
         blocks = -(-cols // CHECKPOINT_BLOCK)
         if scales.shape != (rows, blocks):
             _invalid("scales must hold one byte for each 128 columns of a row")
-        if codes.device != scales.device:
+        if device != scales.device:
             _invalid("codes and scales must be on one device")
-        ld, step = codes.stride()
-        ld_scales, step_scales = scales.stride()
+        strides, strides_scales = codes.stride(), scales.stride()
+        ld, step = strides
+        ld_scales, step_scales = strides_scales
         if (cols > 1 and step != 1) or (blocks > 1 and step_scales != 1):
             _invalid("the rows of codes and scales must be contiguous")
         # a row's codes are written to the next multiple of 16: bytes of that row
@@ -164,8 +169,10 @@ class Checkpoint:
         if rows > 1 and ld_scales % 4 == 0 and rows * ld_scales > \
                 scales.untyped_storage().nbytes() - scales.storage_offset():
             _invalid("the last row of scales must be as long as the others")
-        return lm_checkpoint(codes.data_ptr(), scales.data_ptr(), rows, cols,
-                             ld if rows > 1 else whole, ld_scales if rows > 1 else blocks)
+        p, q = codes.data_ptr(), scales.data_ptr()
+        self._place = lm_checkpoint(p, q, rows, cols, ld if rows > 1 else whole,
+                                    ld_scales if rows > 1 else blocks)
+        self._layout = (p, q, shape, strides, strides_scales)
 
     @property
     def codes(self):
@@ -585,13 +592,11 @@ def lionmuon_grouped_weight_grad(dy, x, offsets, out=None, accumulate=False, str
     if out is None:
         if accumulate:
             _invalid("accumulate needs out")
-        _check_place(offsets, "offsets", device)
-        if offsets.numel() < 2:
-            _invalid("offsets must hold at least two values")
-        experts = offsets.numel() - 1
+        # (no value is one too few for no expert, which the workspace's size refuses)
+        experts = max(offsets.numel() - 1, 0) if isinstance(offsets, torch.Tensor) else 0
         at = _offsets(offsets, experts, device)
         dw = torch.empty((experts, m.cols, cols), dtype=torch.float32, device=device)
-        mo = _stack(dw, "out", device)
+        mo = lm_stack(dw.data_ptr(), experts, m.cols, cols, cols, m.cols * cols, 0, 0)
     else:
         dw, mo = out, _stack(out, "out", device)
         experts = mo.count
